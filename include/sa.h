@@ -55,7 +55,8 @@ typedef enum {
   SA_ERR_CUDA = 4,        /* a CUDA runtime call failed (launch error, no device)       */
   SA_ERR_BAD_PERM = 5,    /* device: perm/inv are not mutually inverse bijections       */
   SA_ERR_TIMEOUT = 6,     /* device: a bounded wait inside a kernel ran out             */
-  SA_ERR_TOO_LARGE = 7    /* sa_make_perm_static: B, n need more than the built-in scratch */
+  SA_ERR_TOO_LARGE = 7,   /* sa_make_perm_static: B, n need more than the built-in scratch */
+  SA_ERR_BAD_CACHE = 8    /* device: a slot, count, length or page outside of an sa_cache   */
 } sa_status;
 
 typedef enum { SA_F32 = 0, SA_BF16 = 1 } sa_dtype;
@@ -317,8 +318,105 @@ sa_status sa_gate_projection_backward(int64_t rows, int32_t dm, int32_t dtype, c
                                       void* dw_swa, void* ws, size_t ws_bytes,
                                       sa_stream_t stream);
 
+/* ---- 4-bit paged cache: what the prefill leaves and single tokens are answered from --------------
+ *
+ * All modes of the paper apply to the prefill; decoding attends over the full KV cache (Sec. 4.2).
+ * These calls hold K and V in 4.5 bits a value, in pages that sequences share, and attend over them.
+ *
+ * Layout.  pool: uint8 [layers, pages, Hkv, 2, page * (d/2 + d/16)].  A page holds `page` tokens; for
+ * each KV head and side (0 = K, 1 = V) first `page` rows of d/2 bytes of codes (dimension 2i in the
+ * low half of byte i), then `page` rows of d/16 scale bytes, one per 16 dimensions.  A value is
+ *     e2m1(code) * e4m3(scale) * t,     t = k_scale or v_scale, a power of two.
+ * Token i of the sequence in table row s lies in page table[s, i / page], row i % page; one table
+ * serves all layers.  lens[s] is the number of its tokens, refs[p] the number of table entries that
+ * name page p (0: free).  Entries of a row are held from the front; -1 behind them.
+ * An empty cache: table all -1, lens and refs 0; pool may hold anything.
+ *
+ * A step of a model:  sa_cache_reserve makes room for the new tokens; per layer sa_cache_append writes
+ * their K and V behind lens and sa_cache_attend reads all; then the caller adds the tokens to lens.
+ *
+ * Lists: `slots` (nullable, device int32 [B]) gives the table row of each sequence of a call, without
+ * it sequence b is row b.  `counts` (nullable, device int32 [B]) gives the new tokens of each sequence,
+ * the first counts[b] of T; what stands behind them is neither read nor written.  Slots of an append
+ * have to be distinct.
+ * Errors of the calls: SA_ERR_INVALID_ARG, SA_ERR_UNSUPPORTED, SA_ERR_WORKSPACE, SA_ERR_CUDA.  What only
+ * the device can see (slots, counts, lengths or pages out of range, a token without a page) is
+ * skipped and recorded as SA_ERR_BAD_CACHE for sa_read_status; keys without a page count as hidden. */
+typedef struct {
+  uint8_t* pool;        /* 16-byte aligned                                                      */
+  int32_t* table;       /* [slots, row]                                                         */
+  int32_t* lens;        /* [slots]                                                              */
+  int32_t* refs;        /* [pages]; only read by reserve, fork, free, compact                   */
+  int32_t layers, pages, Hkv, d;   /* d: a multiple of 16, at most 256                          */
+  int32_t page, slots, row;        /* page: 16, 32, 64 or 128 tokens                            */
+  float k_scale, v_scale;          /* powers of two, 2^-32 .. 2^32                              */
+} sa_cache;
+
+/* Bytes of one page in one layer, all heads, K and V; 0 for a bad geometry.  Host-only. */
+size_t sa_cache_page_bytes(const sa_cache* c);
+
+/* Quantises the new tokens k, v (device, [B,Hkv,T,d] with the given element strides, d contiguous,
+ * dtype SA_F32 or SA_BF16) into a layer, at positions lens[slot] + t.  Per token, head and 16
+ * dimensions, with x over t: scale = e4m3(min(max|x| / 6, 448)), code = e2m1(x / scale) saturating at
+ * 6, both to the nearest with ties to even, decided exactly; 16 values with an infinity or a NaN among
+ * them read back as NaN.  lens is not changed. */
+sa_status sa_cache_append(const sa_cache* c, int32_t layer, int32_t B, int32_t T, const void* k,
+                          const void* v, int32_t dtype, const int64_t kv_stride[3],
+                          const int32_t* slots, const int32_t* counts, sa_stream_t stream);
+
+/* Reads tokens starts[b] + t (starts nullable: from 0), t < counts[b] or T, of a layer back into k, v:
+ * out, [B,Hkv,T,d].  Exact for values within the type.  Reads pages, not lens. */
+sa_status sa_cache_read(const sa_cache* c, int32_t layer, int32_t B, int32_t T, void* k, void* v,
+                        int32_t dtype, const int64_t kv_stride[3], const int32_t* slots,
+                        const int32_t* starts, const int32_t* counts, sa_stream_t stream);
+
+/* Softmax attention (Eq. 1) of the T newest tokens over a layer of the cache.  Token t of sequence b has
+ * position lens[slot] + t and sees key j iff
+ *     j <= position     with SA_CAUSAL: the new tokens' own keys have been appended,
+ *     j <  lens[slot]   without: the cached prefix alone, for joining with the tokens' own attention,
+ *     and position - j < w   if w > 0.
+ * q: [B,Hq,T,d], q_stride; y: out, y_stride; both dtype; rows 16-byte aligned, strides multiples of 8
+ * elements.  lse: out, nullable, contiguous fp32 [B,Hq,T].  A row that sees nothing gets y = 0 and
+ * lse = -infinity.  softmax_scale 0 selects 1/sqrt(d).  flags: 0 or SA_CAUSAL.
+ * ws: scratch of sa_cache_attend_ws_bytes(c, B, T, Hq, dtype) bytes, 16-byte aligned, contents of no
+ * matter; not to be shared by calls that may run at the same time. */
+size_t sa_cache_attend_ws_bytes(const sa_cache* c, int32_t B, int32_t T, int32_t Hq, int32_t dtype);
+sa_status sa_cache_attend(const sa_cache* c, int32_t layer, int32_t B, int32_t T, int32_t Hq,
+                          const void* q, int32_t dtype, const int64_t q_stride[3],
+                          const int32_t* slots, const int32_t* counts, int32_t w, uint32_t flags,
+                          float softmax_scale, void* y, const int64_t y_stride[3], float* lse,
+                          void* ws, size_t ws_bytes, sa_stream_t stream);
+
+/* Frees: every page that a listed slot (device int32 [n]) holds loses a holder, the row becomes -1, its
+ * length 0.  Slots have to be distinct (a second mention is recorded and does nothing). */
+sa_status sa_cache_free(const sa_cache* c, int32_t n, const int32_t* slots, sa_stream_t stream);
+
+/* Forks: child i (an empty slot) gets the pages and the length of parent i; no page is copied, each has
+ * one holder more.  Several children may have one parent.  Recorded and left out: a child that is
+ * listed twice, is a parent as well or holds pages, a parent without the pages of its length. */
+sa_status sa_cache_fork(const sa_cache* c, int32_t n, const int32_t* parents,
+                        const int32_t* children, sa_stream_t stream);
+
+/* Makes room for add[s] tokens (device int32 [slots]) behind lens[s] in every slot: pages that are missing are
+ * taken from the free ones, and pages of that range which others hold too are replaced by a copy of their
+ * own, in all layers, before anything is written to them.  Free pages go out lowest first, to slots in
+ * their order; a slot gets all that it needs or nothing, and once one did not fit none behind it gets any.
+ * A page that all its holders replace in one call is free afterwards, for later calls.
+ * got: out, device int32 [slots]: 1 where the room is there, 0 where it is not (no pages left, or a row
+ * too short).  lens is not changed.  ws: scratch of sa_cache_ws_bytes(c), 16-byte aligned. */
+size_t sa_cache_ws_bytes(const sa_cache* c);
+sa_status sa_cache_reserve(const sa_cache* c, const int32_t* add, int32_t* got, void* ws,
+                           size_t ws_bytes, sa_stream_t stream);
+
+/* Packs the pool: with n pages held, the i-th free page below n takes the contents (all layers), the
+ * holders and the table entries of the i-th held page from n on.  live: out, nullable, device int32 [1]:
+ * n.  Pages from n on are free then, so that the pool's tail can be given up.  ws as for reserve. */
+sa_status sa_cache_compact(const sa_cache* c, int32_t* live, void* ws, size_t ws_bytes,
+                           sa_stream_t stream);
+
 /* Synchronises the stream, returns the device status word (SA_OK, SA_ERR_BAD_PERM or
- * SA_ERR_TIMEOUT) of the current device and clears it. */
+ * SA_ERR_TIMEOUT) of the current device and clears it.  SA_ERR_BAD_CACHE has a word of its own, which is
+ * returned and cleared when the other holds SA_OK; it makes no later call return early. */
 sa_status sa_read_status(sa_stream_t stream);
 
 /* Static, human-readable name of a status code.  Host pointer. */

@@ -3,12 +3,14 @@
 #include <atomic>
 #include <cmath>
 
+#include "sa_cache.cuh"
 #include "sa_common.cuh"
 #include "sa_fwd_tc.cuh"
 
 namespace sa {
 
 __device__ int g_status_word = 0;
+__device__ int g_cache_status_word = 0;
 static std::atomic<uint64_t> g_launches{0};
 static cudaEvent_t g_prof_start = nullptr, g_prof_stop = nullptr;
 
@@ -21,16 +23,24 @@ int debug_option(int key) {
   return key >= 0 && key < SA_DEBUG_KEYS ? g_debug[key].load(std::memory_order_relaxed) : 0;
 }
 
-int* status_ptr() {
-  static std::atomic<int*> ptrs[64];
+// Address of a device word on the current device, looked up once per device.
+static int* word_ptr(std::atomic<int*> (&ptrs)[64], const int& word) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
   int* p = ptrs[dev].load(std::memory_order_acquire);
   if (!p) {
-    if (cudaGetSymbolAddress((void**)&p, g_status_word) != cudaSuccess) return nullptr;
+    if (cudaGetSymbolAddress((void**)&p, word) != cudaSuccess) return nullptr;
     ptrs[dev].store(p, std::memory_order_release);
   }
   return p;
+}
+int* status_ptr() {
+  static std::atomic<int*> ptrs[64];
+  return word_ptr(ptrs, g_status_word);
+}
+int* cache_status_ptr() {
+  static std::atomic<int*> ptrs[64];
+  return word_ptr(ptrs, g_cache_status_word);
 }
 
 namespace {
@@ -445,6 +455,10 @@ sa_status sa_read_status(sa_stream_t stream) {
   if (!p) return SA_ERR_CUDA;
   int host = 0;
   if (cudaMemcpy(&host, p, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return SA_ERR_CUDA;
+  if (host == 0) {                       // the cache's calls have a word of their own
+    if (!(p = cache_status_ptr())) return SA_ERR_CUDA;
+    if (cudaMemcpy(&host, p, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return SA_ERR_CUDA;
+  }
   if (host != 0) {
     const int zero = 0;
     if (cudaMemcpy(p, &zero, sizeof(int), cudaMemcpyHostToDevice) != cudaSuccess)
@@ -463,6 +477,7 @@ const char* sa_status_string(sa_status s) {
     case SA_ERR_BAD_PERM: return "perm/inv are not mutually inverse permutations";
     case SA_ERR_TIMEOUT: return "a bounded device-side wait ran out";
     case SA_ERR_TOO_LARGE: return "B*n needs more scratch than sa_make_perm_static has built in";
+    case SA_ERR_BAD_CACHE: return "a slot, count, length or page outside of the cache";
     default: return "unknown status";
   }
 }
