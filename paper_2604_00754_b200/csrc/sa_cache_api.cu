@@ -51,7 +51,7 @@ sa_status check_rows(const sa_cache* c, int32_t layer, int32_t B, int32_t T, int
   if (!power_of_two(c->k_scale) || !power_of_two(c->v_scale)) return SA_ERR_INVALID_ARG;
   if (layer < 0 || layer >= c->layers || B < 1 || T < 1) return SA_ERR_INVALID_ARG;
   if (dtype != SA_F32 && dtype != SA_BF16) return SA_ERR_INVALID_ARG;
-  if (B > 65535 || T > (1 << 30)) return SA_ERR_UNSUPPORTED;
+  if (B > 65535 || T > (1 << 28)) return SA_ERR_UNSUPPORTED;
   return SA_OK;
 }
 
@@ -94,7 +94,8 @@ bool good_heads(const sa_cache* c, int32_t Hq) { return Hq >= c->Hkv && Hq % c->
 
 // Row tiles of all sequences are counted in 32 bits.
 bool attend_fits(const sa_cache* c, int32_t B, int32_t T, int32_t Hq) {
-  return ((int64_t)Hq / c->Hkv * T / 8 + 1) * B < (1ll << 30);
+  const int64_t rows = (int64_t)Hq / c->Hkv * T;
+  return rows < (1ll << 30) && (rows / 8 + 1) * B < (1ll << 30);
 }
 
 }  // namespace

@@ -1,137 +1,14 @@
-// Attention of a sequence's newest tokens over its 4-bit cache.
-//
-// The query rows of a KV head (its G query heads times the T new tokens) are cut into tiles of kRows;
-// an entry is a sequence and a row tile, a segment an entry and a KV head, a step 64 of its keys.
-// All steps stand in one line, segment after segment, and each CTA takes an equal share of it,
-// whatever the lengths are: the lengths are known to the device alone, and a batch of uneven ones fills
-// the GPU as an even one does.  A segment that lies within one share is finished there; of one that
-// does not, each share leaves maximum, sum and unnormalised rows in the workspace, and the second launch
-// joins them in the order of the shares (so results do not depend on timing).
-//
-// This kernel takes any head dimension and computes on the CUDA cores in fp32.
-#include <algorithm>
-
-#include "sa_cache.cuh"
+// Attention of a sequence's newest tokens over its 4-bit cache: the kernel for any head dimension, on the
+// CUDA cores in fp32, the launch that joins split segments, and the choice between the kernels.
+// sa_cache_attend.cuh says how the work is cut.
+#include "sa_cache_attend.cuh"
 
 namespace sa {
+using namespace attend;
 namespace {
 
-constexpr int kStep = 64;      // keys per step
-constexpr int kUnit = 16;      // keys a warp takes of a step; pages hold a multiple of it
-constexpr int kWarps = 4;
-constexpr int kRows = 8;       // query rows of a tile
-constexpr int kShares = 4 * 148;  // CTAs: four per SM
-
-// A split segment, filed under the share that begins it.
-struct Split {
-  int e, h, parts, pad;
-};
-
-struct Params {
-  AttendArgs a;
-  int G, tiles, entries;  // query heads per KV head, row tiles of a sequence, all entries
-  float* part;            // [kShares][2][kRows * (d + 2)]: a share's first and last segment
-  Split* split;           // [kShares]
-  float scale2;           // scores times log2(e), K's power of two folded in
-};
-
-// Keys [lo, hi) that the rows of an entry may see, in steps [first, first + n); n = 0: no rows.
-struct Entry {
-  int b, slot, len, r0, rows, lo, hi, first, n;
-};
-
-__device__ Entry entry(const Params& p, int e) {
-  const AttendArgs& a = p.a;
-  Entry r{};
-  r.b = e / p.tiles;
-  r.r0 = (e - r.b * p.tiles) * kRows;
-  const int count = cache_count(a.c, a.counts, r.b, a.T);
-  if (count <= 0 || r.r0 >= p.G * count) return r;
-  r.slot = cache_slot(a.c, a.slots, r.b);
-  if (r.slot < 0) return r;
-  r.len = a.c.lens[r.slot];
-  const int64_t most = (int64_t)a.c.row * a.c.P;
-  if (r.len < 0 || r.len > most) {
-    report_cache(a.c);
-    return r;
-  }
-  r.rows = min(kRows, p.G * count - r.r0);
-  const int t0 = r.r0 / p.G, t1 = (r.r0 + r.rows - 1) / p.G;
-  int64_t hi = a.causal ? (int64_t)r.len + t1 + 1 : r.len;
-  if (hi > most) {
-    report_cache(a.c);
-    hi = most;
-  }
-  r.hi = (int)hi;
-  r.lo = a.w > 0 ? min((int)max((int64_t)r.len + t0 - a.w + 1, (int64_t)0), r.hi) : 0;
-  r.first = r.lo / kStep;
-  r.n = max((r.hi + kStep - 1) / kStep - r.first, 1);   // one step at least: empty rows are written too
-  return r;
-}
-
-// Where the line of steps is cut: share i takes [total * i / shares, total * (i + 1) / shares).
-struct Line {
-  int64_t total;
-  int shares;
-  __device__ int64_t begin(int i) const { return total * i / shares; }
-  // the share that holds step s
-  __device__ int of(int64_t s) const { return (int)(((s + 1) * shares - 1) / total); }
-};
-
-// The line, and the entry that holds the first step of share `blockIdx.x` with the steps before that
-// entry.  Each thread adds up a run of entries; one scan of the runs' sums.  All threads call it.
-__device__ Line find(const Params& p, int* e_out, int64_t* before_out) {
-  __shared__ int64_t sums[kWarps];
-  __shared__ int64_t found_before;
-  __shared__ int found;
-  const int tid = threadIdx.x, threads = 32 * kWarps;
-  const int run = (p.entries + threads - 1) / threads;
-  const int e0 = min(tid * run, p.entries), e1 = min(e0 + run, p.entries);
-  int64_t mine = 0;
-  for (int e = e0; e < e1; ++e) mine += entry(p, e).n;
-  mine *= p.a.c.Hkv;
-  int64_t upto = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
-    if ((tid & 31) >= o) upto += v;
-  }
-  if ((tid & 31) == 31) sums[tid >> 5] = upto;
-  if (tid == 0) found = -1;
-  __syncthreads();
-  Line line{0, 1};
-  for (int i = 0; i < kWarps; ++i) {
-    if (i < (tid >> 5)) upto += sums[i];
-    line.total += sums[i];
-  }
-  line.shares = (int)min((int64_t)kShares, line.total);
-  if ((int)blockIdx.x < line.shares) {
-    const int64_t s = line.begin(blockIdx.x);
-    int64_t at = upto - mine;
-    if (s >= at && s < upto)
-      for (int e = e0; e < e1; ++e) {
-        const int64_t n = (int64_t)entry(p, e).n * p.a.c.Hkv;
-        if (s < at + n) {
-          found = e;
-          found_before = at;
-          break;
-        }
-        at += n;
-      }
-  }
-  __syncthreads();
-  *e_out = found;
-  *before_out = found_before;
-  return line;
-}
-
-// One row of the result: o over its sum, and the log-sum-exp; m in log2 units, the sum relative to it.
-__device__ __forceinline__ float row_lse(float m, float l) {
-  return l > 0.f || l != l ? (m + log2f(l)) * kLn2 : -INFINITY;
-}
-__device__ __forceinline__ float row_scale(float l, float v_scale) {
-  return l > 0.f || l != l ? v_scale / l : 0.f;
-}
+constexpr int kRows = 8;          // query rows of a tile of this kernel
+constexpr int kShares = 2 * 148;  // its CTAs: two per SM (217 registers)
 
 template <typename T>
 __global__ void __launch_bounds__(32 * kWarps) attend_kernel(const Params p) {
@@ -155,7 +32,6 @@ __global__ void __launch_bounds__(32 * kWarps) attend_kernel(const Params p) {
   int64_t s = line.begin(blockIdx.x);
   const int64_t end = line.begin(blockIdx.x + 1);
   Split mine{0, 0, 0, 0};
-  bool first = true;
   Entry en = entry(p, e);
   while (s < end) {
     while (en.n == 0 || s >= before + (int64_t)en.n * c.Hkv) {
@@ -169,11 +45,7 @@ __global__ void __launch_bounds__(32 * kWarps) attend_kernel(const Params p) {
     for (int i = tid; i < kRows * d; i += 32 * kWarps) {
       const int r = i / d, x = i - r * d;
       float v = 0.f;
-      if (r < en.rows) {
-        const int t = (en.r0 + r) / p.G, g = (en.r0 + r) - t * p.G;
-        v = to_f32(reinterpret_cast<const T*>(a.q)[en.b * a.qs[0] + (int64_t)(h * p.G + g) * a.qs[1] +
-                                                   (int64_t)t * a.qs[2] + x]);
-      }
+      if (r < en.rows) v = to_f32(row_of(p, reinterpret_cast<const T*>(a.q), a.qs, en, h, r)[x]);
       q_s[i] = v;
     }
     __syncthreads();
@@ -277,12 +149,8 @@ __global__ void __launch_bounds__(32 * kWarps) attend_kernel(const Params p) {
     }
     __syncthreads();
     const bool whole = k0 == 0 && k1 == en.n;
-    float* part = p.part + ((int64_t)blockIdx.x * 2 + (first ? 0 : 1)) * kRows * (d + 2);
-    if (!whole && k0 == 0) {
-      // filed by the share that begins it; the others' parts are their first segments
-      part = p.part + ((int64_t)blockIdx.x * 2 + 1) * kRows * (d + 2);
-      mine = Split{e, h, line.of(seg + en.n - 1) - (int)blockIdx.x + 1, 0};
-    }
+    float* part = part_of(p, blockIdx.x, k0 == 0);
+    if (!whole && k0 == 0) mine = Split{e, h, line.of(seg + en.n - 1) - (int)blockIdx.x + 1, 0};
     for (int i = tid; i < en.rows * d; i += 32 * kWarps) {
       const int r = i / d, x = i - r * d;
       float to = -INFINITY;
@@ -297,10 +165,8 @@ __global__ void __launch_bounds__(32 * kWarps) attend_kernel(const Params p) {
         v += keep * o_s[(w * kRows + r) * d + x];
       }
       if (whole) {
-        const int t = (en.r0 + r) / p.G, g = (en.r0 + r) - t * p.G, hq = h * p.G + g;
-        reinterpret_cast<T*>(a.y)[en.b * a.ys[0] + hq * a.ys[1] + (int64_t)t * a.ys[2] + x] =
-            from_f32<T>(v * row_scale(sum, c.v_scale));
-        if (x == 0 && a.lse) a.lse[((int64_t)en.b * a.Hq + hq) * a.T + t] = row_lse(to, sum);
+        row_of(p, reinterpret_cast<T*>(a.y), a.ys, en, h, r)[x] = from_f32<T>(v * row_scale(sum, c.v_scale));
+        if (x == 0 && a.lse) *lse_of(p, en, h, r) = row_lse(to, sum);
       } else {
         part[r * d + x] = v;
         if (x == 0) {
@@ -310,7 +176,6 @@ __global__ void __launch_bounds__(32 * kWarps) attend_kernel(const Params p) {
       }
     }
     s = seg + k1;
-    first = false;
   }
   if (tid == 0) p.split[blockIdx.x] = mine;
 }
@@ -326,12 +191,10 @@ __global__ void __launch_bounds__(32 * kWarps) join_kernel(const Params p) {
   if (sp.parts == 0) return;
   const Entry en = entry(p, sp.e);
   if (r >= en.rows) return;
-  const int stride = kRows * (d + 2);
-  auto part = [&](int i) {
-    return p.part + ((int64_t)(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * stride;
-  };
+  const int rows = p.rows;
+  auto part = [&](int i) { return part_of(p, blockIdx.x + i, i == 0); };
   float to = -INFINITY;
-  for (int i = tid; i < sp.parts; i += 32 * kWarps) to = fmaxf(to, part(i)[kRows * d + r]);
+  for (int i = tid; i < sp.parts; i += 32 * kWarps) to = fmaxf(to, part(i)[rows * d + r]);
   __shared__ float tops[kWarps];
   to = warp_max(to);
   if (lane == 0) tops[warp] = to;
@@ -343,8 +206,8 @@ __global__ void __launch_bounds__(32 * kWarps) join_kernel(const Params p) {
   float v[8] = {}, sum = 0.f;
   for (int i = warp; i < sp.parts; i += kWarps) {
     const float* f = part(i);
-    const float keep = exp2f(f[kRows * d + r] - ref);
-    sum += keep * f[kRows * (d + 1) + r];
+    const float keep = exp2f(f[rows * d + r] - ref);
+    sum += keep * f[rows * (d + 1) + r];
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (lane + 32 * j < d) v[j] += keep * f[r * d + lane + 32 * j];
@@ -357,45 +220,54 @@ __global__ void __launch_bounds__(32 * kWarps) join_kernel(const Params p) {
   sum = 0.f;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) sum += smem[w * (d + 1) + d];
-  const int t = (en.r0 + r) / p.G, g = (en.r0 + r) - t * p.G, hq = sp.h * p.G + g;
+  T* y = row_of(p, reinterpret_cast<T*>(a.y), a.ys, en, sp.h, r);
   for (int x = tid; x < d; x += 32 * kWarps) {
     float o = 0.f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) o += smem[w * (d + 1) + x];
-    reinterpret_cast<T*>(a.y)[en.b * a.ys[0] + hq * a.ys[1] + (int64_t)t * a.ys[2] + x] =
-        from_f32<T>(o * row_scale(sum, a.c.v_scale));
+    y[x] = from_f32<T>(o * row_scale(sum, a.c.v_scale));
   }
-  if (tid == 0 && a.lse) a.lse[((int64_t)en.b * a.Hq + hq) * a.T + t] = row_lse(to, sum);
+  if (tid == 0 && a.lse) *lse_of(p, en, sp.h, r) = row_lse(to, sum);
 }
 
 template <typename T>
 cudaError_t launch(const Params& p, cudaStream_t st) {
   const int d = p.a.c.d;
   const size_t smem = 4 * (size_t)(kRows * d + kWarps * kUnit * kRows + kWarps * kRows * d + kWarps * 2 * kRows);
-  bump_launches();
-  cudaError_t e = launch_dependent(attend_kernel<T>, dim3(kShares), dim3(32 * kWarps), smem, st, p);
-  if (e != cudaSuccess) return e;
-  bump_launches();
-  return launch_dependent(join_kernel<T>, dim3(kShares, kRows), dim3(32 * kWarps),
-                          4 * (size_t)kWarps * (d + 1), st, p);
+  return launch_dependent(attend_kernel<T>, dim3(p.shares), dim3(32 * kWarps), smem, st, p);
 }
 
 }  // namespace
 
+cudaError_t launch_cache_join(const Params& p, int dtype, cudaStream_t st) {
+  const dim3 grid(p.shares, p.rows);
+  const size_t smem = 4 * (size_t)kWarps * (p.a.c.d + 1);
+  bump_launches();
+  return dtype == SA_BF16 ? launch_dependent(join_kernel<__nv_bfloat16>, grid, dim3(32 * kWarps), smem, st, p)
+                          : launch_dependent(join_kernel<float>, grid, dim3(32 * kWarps), smem, st, p);
+}
+
+static void shape(int T, int G, int d, int dtype, int* shares, int* rows) {
+  if (cache_attend_mma_takes(d)) return cache_attend_mma_shape(T, G, d, dtype, shares, rows);
+  *shares = kShares;
+  *rows = kRows;
+}
+
 size_t cache_attend_ws_bytes(int B, int T, int Hq, int Hkv, int d, int dtype) {
-  return (size_t)kShares * (2 * kRows * (d + 2) * 4 + sizeof(Split));
+  int shares, rows;
+  shape(T, Hq / Hkv, d, dtype, &shares, &rows);
+  return attend::ws_bytes(shares, rows, d);
 }
 
 cudaError_t launch_cache_attend(const AttendArgs& a, int dtype, cudaStream_t st) {
-  Params p{};
-  p.a = a;
-  p.G = a.Hq / a.c.Hkv;
-  p.tiles = (p.G * a.T + kRows - 1) / kRows;
-  p.entries = a.B * p.tiles;
-  p.split = (Split*)a.ws;
-  p.part = (float*)(p.split + kShares);
-  p.scale2 = a.scale * kLog2e * a.c.k_scale;
-  return dtype == SA_BF16 ? launch<__nv_bfloat16>(p, st) : launch<float>(p, st);
+  int shares, rows;
+  shape(a.T, a.Hq / a.c.Hkv, a.c.d, dtype, &shares, &rows);
+  const Params p = attend::params(a, shares, rows);
+  bump_launches();
+  const cudaError_t e = cache_attend_mma_takes(a.c.d) ? launch_cache_attend_mma(p, dtype, st)
+                        : dtype == SA_BF16            ? launch<__nv_bfloat16>(p, st)
+                                                      : launch<float>(p, st);
+  return e == cudaSuccess ? launch_cache_join(p, dtype, st) : e;
 }
 
 }  // namespace sa
