@@ -571,102 +571,17 @@ def sa_cache_pool(layers: int, pages: int, Hkv: int, page: int, d: int, device="
     return torch.empty(layers, pages, Hkv, 2, page * (d // 2 + d // 16), dtype=torch.uint8, device=device)
 
 
-def _ints(t: torch.Tensor, shape, what: str, like: torch.Tensor):
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous() \
-            or t.device != like.device:
-        raise ValueError("%s must be contiguous int32 %s on the cache's device" % (what, list(shape)))
-
-
-def _cache(pool, table, lens, refs, page: int, d: int, k_scale=1.0, v_scale=1.0) -> SaCache:
-    """Describes a cache to the library.  Without a pool (the books alone) d is any valid one."""
-    if table.dim() != 2:
-        raise ValueError("table must be [slots, row]")
-    slots, row = table.shape
-    _ints(table, (slots, row), "table", table)
-    c = SaCache(table=table.data_ptr(), layers=1, pages=1, Hkv=1, d=d, page=page, slots=slots, row=row,
-                k_scale=k_scale, v_scale=v_scale)
-    if lens is not None:
-        _ints(lens, (slots,), "lens", table)
-        c.lens = lens.data_ptr()
-    if pool is not None:
-        if pool.dtype != torch.uint8 or pool.dim() != 5 or pool.shape[3] != 2 or not pool.is_contiguous() \
-                or pool.device != table.device or pool.shape[4] != page * (d // 2 + d // 16):
-            raise ValueError("pool must be contiguous uint8 [layers, pages, Hkv, 2, page * (d/2 + d/16)] "
-                             "on the table's device")
-        c.pool, c.layers, c.pages, c.Hkv = pool.data_ptr(), pool.shape[0], pool.shape[1], pool.shape[2]
-    if refs is not None:
-        if pool is None:
-            c.pages = refs.numel()
-        _ints(refs, (c.pages,), "refs", table)
-        c.refs = refs.data_ptr()
-    return c
-
-
-def _page_of(pool, d: int) -> int:
-    return pool.shape[4] * 16 // (9 * d) if pool.dim() == 5 and d else 0
-
-
-def _rows_dtype(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype == torch.bfloat16:
-        return BF16
-    raise TypeError("tensors must be float32 or bfloat16")
-
-
-def _strides(t: torch.Tensor):
-    if t.stride(3) != 1:
-        raise ValueError("the head dimension must be contiguous")
-    # a dimension of one may have any stride
-    return (ctypes.c_int64 * 3)(*(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)))
-
-
-def _written(t: torch.Tensor, what: str):
-    """Refuses an output whose elements share memory (an expanded tensor)."""
-    if any(t.shape[i] > 1 and t.stride(i) == 0 for i in range(3)):
-        raise ValueError("%s shares memory between its rows" % what)
-
-
-def _kv_rows(k, v, pool, table, lens, layer, lists, k_scale, v_scale):
-    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.device != pool.device \
-            or v.device != pool.device:
-        raise ValueError("k and v must be [B,Hkv,T,d] of one type on the cache's device")
-    B, Hkv, T, d = k.shape
-    st = _strides(k)
-    if list(st) != list(_strides(v)):
-        raise ValueError("k and v must share their strides")
-    c = _cache(pool, table, lens, None, _page_of(pool, d), d, k_scale, v_scale)
-    if Hkv != c.Hkv:
-        raise ValueError("k and v must have the pool's %d heads" % c.Hkv)
-    for name, t in lists.items():
-        if t is not None:
-            _ints(t, (B,), name, table)
-    return ctypes.byref(c), int(layer), B, T, st
-
-
 def sa_cache_append(pool, table, lens, k, v, layer=0, slots=None, counts=None, k_scale=2.0 ** -4,
                     v_scale=2.0 ** -4):
     """Quantises k, v ([B,Hkv,T,d]) into a layer, token t of sequence b at position lens[slot] + t.
     slots, counts: int32 [B] or None (row b; all T).  Pages must be there (sa_cache_reserve); lens stays."""
-    lib = load_library()
-    c, layer, B, T, st = _kv_rows(k, v, pool, table, lens, layer, dict(slots=slots, counts=counts), k_scale, v_scale)
-    with torch.cuda.device(pool.device):
-        _check(lib.sa_cache_append(c, layer, B, T, _ptr(k), _ptr(v), _rows_dtype(k), st, _ptr(slots), _ptr(counts),
-                                   _stream()), "sa_cache_append")
+    return (_nat or load_native()).cache_append(pool, table, lens, k, v, layer, slots, counts, k_scale, v_scale)
 
 
 def sa_cache_read(pool, table, k, v, layer=0, slots=None, starts=None, counts=None, k_scale=2.0 ** -4,
                   v_scale=2.0 ** -4):
     """Reads tokens starts[b] + t (from 0 without starts) back into k, v ([B,Hkv,T,d]); returns them."""
-    lib = load_library()
-    _written(k, "k")
-    _written(v, "v")
-    c, layer, B, T, st = _kv_rows(k, v, pool, table, None, layer, dict(slots=slots, starts=starts, counts=counts),
-                                  k_scale, v_scale)
-    with torch.cuda.device(pool.device):
-        _check(lib.sa_cache_read(c, layer, B, T, _ptr(k), _ptr(v), _rows_dtype(k), st, _ptr(slots), _ptr(starts),
-                                 _ptr(counts), _stream()), "sa_cache_read")
-    return k, v
+    return (_nat or load_native()).cache_read(pool, table, k, v, layer, slots, starts, counts, k_scale, v_scale)
 
 
 def sa_cache_attend(pool, table, lens, q, layer=0, slots=None, counts=None, w=0, flags=CAUSAL, scale=0.0,
@@ -676,97 +591,29 @@ def sa_cache_attend(pool, table, lens, q, layer=0, slots=None, counts=None, w=0,
     Token t has position lens[slot] + t; it sees the keys up to its own (CAUSAL, the new tokens appended) or
     those before lens (flags 0), of them the last w if w > 0.  A row without keys: y = 0, lse = -inf.
     Rows t >= counts[b] of y and lse are left as they were (a fresh y: undefined)."""
-    lib = load_library()
-    if q.dim() != 4 or q.device != pool.device:
-        raise ValueError("q must be [B,Hq,T,d] on the cache's device")
-    B, Hq, T, d = q.shape
-    c = _cache(pool, table, lens, None, _page_of(pool, d), d, k_scale, v_scale)
-    dt = _rows_dtype(q)
-    for name, t in (("slots", slots), ("counts", counts)):
-        if t is not None:
-            _ints(t, (B,), name, table)
-    if y is None:
-        y = torch.empty(B, Hq, T, d, dtype=q.dtype, device=q.device)
-    elif y.shape != q.shape or y.dtype != q.dtype or y.device != q.device:
-        raise ValueError("y must have the shape and type of q")
-    else:
-        _written(y, "y")
-    if lse is None and want_lse:
-        lse = torch.empty(B, Hq, T, dtype=torch.float32, device=q.device)
-    elif lse is not None and (tuple(lse.shape) != (B, Hq, T) or lse.dtype != torch.float32
-                              or not lse.is_contiguous() or lse.device != q.device):
-        raise ValueError("lse must be contiguous float32 [B,Hq,T]")
-    need = int(lib.sa_cache_attend_ws_bytes(ctypes.byref(c), B, T, Hq, dt))
-    if need == ctypes.c_size_t(-1).value:
-        raise SaError(1, "sa_cache_attend")
-    with torch.cuda.device(pool.device):
-        ws = _workspace(need, q.device, ws)
-        _check(lib.sa_cache_attend(ctypes.byref(c), int(layer), B, T, Hq, _ptr(q), dt, _strides(q), _ptr(slots),
-                                   _ptr(counts), int(w), int(flags), float(scale), _ptr(y), _strides(y), _ptr(lse),
-                                   _ptr(ws), ws.numel(), _stream()), "sa_cache_attend")
-    return (y, lse) if lse is not None else y
-
-
-def _books_call(name, table, n_lists, c, *args):
-    n = n_lists[0].numel()
-    for t in n_lists:
-        _ints(t, (n,), "slot lists", table)
-    with torch.cuda.device(table.device):
-        _check(getattr(load_library(), name)(ctypes.byref(c), n, *(_ptr(t) for t in n_lists), _stream()), name)
+    return (_nat or load_native()).cache_attend(pool, table, lens, q, layer, slots, counts, w, flags, scale,
+                                                k_scale, v_scale, y, want_lse, lse, ws)
 
 
 def sa_cache_free(table, lens, refs, slots):
     """Empties the listed slots (int32 [n]): their pages lose a holder."""
-    _books_call("sa_cache_free", table, (slots,), _cache(None, table, lens, refs, 16, 16))
+    return (_nat or load_native()).cache_free(table, lens, refs, slots)
 
 
 def sa_cache_fork(table, lens, refs, parents, children, page: int):
     """children[i] (empty slots) share the pages of parents[i] (int32 [n] each); page: tokens per page."""
-    if children.shape != parents.shape:
-        raise ValueError("parents and children must have one length")
-    _books_call("sa_cache_fork", table, (parents, children), _cache(None, table, lens, refs, page, 16))
-
-
-def _books_ws(c, device, ws):
-    need = int(load_library().sa_cache_ws_bytes(ctypes.byref(c)))
-    if need == ctypes.c_size_t(-1).value:
-        raise SaError(1, "sa_cache_ws_bytes")
-    return _workspace(need, device, ws)
-
-
-def _head_dim(pool, page: int) -> int:
-    return pool.shape[4] * 16 // (9 * page) if pool.dim() == 5 and page else 0
+    return (_nat or load_native()).cache_fork(table, lens, refs, parents, children, page)
 
 
 def sa_cache_reserve(pool, table, lens, refs, add, page: int, got=None, ws=None):
     """Makes room for add[s] tokens (int32 [slots]) behind lens[s]: pages taken, shared ones copied.
     Returns got, int32 [slots]: 1 where the room is there."""
-    c = _cache(pool, table, lens, refs, page, _head_dim(pool, page))
-    _ints(add, (c.slots,), "add", table)
-    with torch.cuda.device(pool.device):
-        got = torch.empty_like(add) if got is None else got
-        _ints(got, (c.slots,), "got", table)
-        ws = _books_ws(c, pool.device, ws)
-        _check(load_library().sa_cache_reserve(ctypes.byref(c), _ptr(add), _ptr(got), _ptr(ws), ws.numel(),
-                                               _stream()), "sa_cache_reserve")
-    return got
+    return (_nat or load_native()).cache_reserve(pool, table, lens, refs, add, page, got, ws)
 
 
 def sa_cache_compact(pool, table, refs, live=None, ws=None):
     """Moves the held pages to the front of the pool; returns their number (int32 [1], on the device)."""
-    # any page size and head dimension with the pool's bytes describe the moves
-    if pool.dim() != 5:
-        raise ValueError("pool must be [layers, pages, Hkv, 2, bytes]")
-    page = next((p for p in (128, 64, 32, 16)
-                 if pool.shape[4] % (9 * p) == 0 and 16 <= _head_dim(pool, p) <= 256), 16)
-    c = _cache(pool, table, None, refs, page, _head_dim(pool, page))
-    with torch.cuda.device(pool.device):
-        live = torch.empty(1, dtype=torch.int32, device=pool.device) if live is None else live
-        _ints(live, (1,), "live", table)
-        ws = _books_ws(c, pool.device, ws)
-        _check(load_library().sa_cache_compact(ctypes.byref(c), _ptr(live), _ptr(ws), ws.numel(), _stream()),
-               "sa_cache_compact")
-    return live
+    return (_nat or load_native()).cache_compact(pool, table, refs, live, ws)
 
 
 def sa_read_status() -> int:

@@ -10,6 +10,7 @@
 #include <ATen/EmptyTensor.h>
 #include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -289,6 +290,251 @@ PyObject* backward(PyObject* const* a) {
   return tuple({dq.result(), dk.result(), dv.result(), gate ? dgate.result() : pass(Py_None)});
 }
 
+// ---- 4-bit paged cache ----
+
+void ints(const at::Tensor* t, at::IntArrayRef sizes, const at::Tensor& like, const char* text) {
+  if (t && (t->scalar_type() != at::kInt || t->sizes() != sizes || !t->is_contiguous() ||
+            t->device() != like.device()))
+    raise(PyExc_ValueError, text);
+}
+int32_t* int_ptr(const at::Tensor* t) { return t ? (int32_t*)t->data_ptr() : nullptr; }
+
+// The cache that pool, table, lens and refs (nullable: not needed) describe.  Without a pool, the books
+// alone, any head dimension is valid.
+sa_cache cache(const at::Tensor* pool, const at::Tensor& table, const at::Tensor* lens,
+               const at::Tensor* refs, int64_t page, int64_t d) {
+  if (table.dim() != 2 || table.scalar_type() != at::kInt || !table.is_contiguous())
+    raise(PyExc_ValueError, "table must be contiguous int32 [slots, row]");
+  sa_cache c{};
+  c.k_scale = c.v_scale = 1.f;
+  c.layers = c.pages = c.Hkv = 1;
+  c.d = (int32_t)d;
+  c.page = (int32_t)page;
+  c.slots = (int32_t)table.size(0);
+  c.row = (int32_t)table.size(1);
+  c.table = int_ptr(&table);
+  ints(lens, {table.size(0)}, table, "lens must be contiguous int32 [slots] on the table's device");
+  c.lens = int_ptr(lens);
+  if (pool) {
+    if (pool->scalar_type() != at::kByte || pool->dim() != 5 || pool->size(3) != 2 || !pool->is_contiguous() ||
+        pool->device() != table.device() || pool->size(4) != page * (d / 2 + d / 16))
+      raise(PyExc_ValueError,
+            "pool must be contiguous uint8 [layers, pages, Hkv, 2, page * (d/2 + d/16)] on the table's device");
+    c.pool = (uint8_t*)pool->data_ptr();
+    c.layers = (int32_t)pool->size(0);
+    c.pages = (int32_t)pool->size(1);
+    c.Hkv = (int32_t)pool->size(2);
+  } else if (refs) {
+    c.pages = (int32_t)refs->numel();
+  }
+  ints(refs, {c.pages}, table, "refs must be contiguous int32 [pages] on the table's device");
+  c.refs = int_ptr(refs);
+  return c;
+}
+
+int64_t page_of(const at::Tensor& pool, int64_t d) { return pool.dim() == 5 && d ? pool.size(4) * 16 / (9 * d) : 0; }
+
+int rows_dtype(const at::Tensor& t) {
+  if (t.scalar_type() == at::kFloat) return SA_F32;
+  if (t.scalar_type() == at::kBFloat16) return SA_BF16;
+  raise(PyExc_TypeError, "tensors must be float32 or bfloat16");
+}
+
+// Element strides of [B,H,T,d]; a dimension of one may have any, an output none of 0 otherwise.
+struct Strides {
+  int64_t s[3];
+};
+Strides row_strides(const at::Tensor& t, bool written) {
+  if (t.stride(3) != 1) raise(PyExc_ValueError, "the head dimension must be contiguous");
+  Strides r;
+  for (int i = 0; i < 3; ++i) {
+    r.s[i] = t.size(i) > 1 ? t.stride(i) : 0;
+    if (written && t.size(i) > 1 && t.stride(i) == 0)
+      raise(PyExc_ValueError, "an output shares memory between its rows");
+  }
+  return r;
+}
+
+void on_gpu(const at::Tensor& t) {
+  if (!t.is_cuda()) raise(PyExc_ValueError, "the cache must be on a CUDA device");
+}
+
+at::Tensor scratch(PyObject* given, size_t need, const at::Tensor& like, const char* where, size_t* bytes,
+                   void** at) {
+  if (need == (size_t)-1) check(SA_ERR_INVALID_ARG, where);
+  on_gpu(like);
+  at::Tensor own;
+  const at::Tensor* ws = tensor_or_null(given);
+  if (!ws) ws = &(own = fresh({(int64_t)need}, at::kByte, like.device()));
+  else if (ws->device() != like.device() || !ws->is_contiguous())
+    raise(PyExc_ValueError, "ws must be contiguous on the cache's device");
+  *bytes = ws->numel() * ws->element_size();
+  *at = ws->data_ptr();
+  return own;
+}
+
+// What append and read share: their checks, and the cache.
+struct Rows {
+  sa_cache c;
+  Strides st;
+  int32_t B, T;
+};
+Rows rows(const at::Tensor& pool, const at::Tensor& table, const at::Tensor* lens, const at::Tensor& k,
+          const at::Tensor& v, std::initializer_list<const at::Tensor*> lists, PyObject* k_scale,
+          PyObject* v_scale, bool written) {
+  if (k.dim() != 4 || v.sizes() != k.sizes() || v.scalar_type() != k.scalar_type() ||
+      k.device() != pool.device() || v.device() != pool.device())
+    raise(PyExc_ValueError, "k and v must be [B,Hkv,T,d] of one type on the cache's device");
+  Rows r;
+  r.st = row_strides(k, written);
+  const Strides sv = row_strides(v, written);
+  for (int i = 0; i < 3; ++i)
+    if (r.st.s[i] != sv.s[i]) raise(PyExc_ValueError, "k and v must share their strides");
+  r.B = (int32_t)k.size(0);
+  r.T = (int32_t)k.size(2);
+  r.c = cache(&pool, table, lens, nullptr, page_of(pool, k.size(3)), k.size(3));
+  r.c.k_scale = (float)real(k_scale);
+  r.c.v_scale = (float)real(v_scale);
+  if (k.size(1) != r.c.Hkv) raise(PyExc_ValueError, "k and v must have the pool's heads");
+  for (const at::Tensor* t : lists)
+    ints(t, {k.size(0)}, table, "slots, starts and counts must be contiguous int32 [B] on the cache's device");
+  on_gpu(pool);
+  return r;
+}
+
+// cache_append(pool, table, lens, k, v, layer, slots, counts, k_scale, v_scale)
+PyObject* cache_append(PyObject* const* a) {
+  const at::Tensor &pool = tensor(a[0]), &k = tensor(a[3]), &v = tensor(a[4]);
+  const at::Tensor *slots = tensor_or_null(a[6]), *counts = tensor_or_null(a[7]);
+  const Rows r = rows(pool, tensor(a[1]), &tensor(a[2]), k, v, {slots, counts}, a[8], a[9], false);
+  const c10::cuda::CUDAGuard guard(pool.device());
+  check(unlocked(sa_cache_append, &r.c, (int32_t)integer(a[5]), r.B, r.T, ptr(k), ptr(v), rows_dtype(k), r.st.s,
+                 int_ptr(slots), int_ptr(counts), stream()),
+        "sa_cache_append");
+  return pass(Py_None);
+}
+
+// cache_read(pool, table, k, v, layer, slots, starts, counts, k_scale, v_scale)
+PyObject* cache_read(PyObject* const* a) {
+  const at::Tensor &pool = tensor(a[0]), &k = tensor(a[2]), &v = tensor(a[3]);
+  const at::Tensor *slots = tensor_or_null(a[5]), *starts = tensor_or_null(a[6]), *counts = tensor_or_null(a[7]);
+  const Rows r = rows(pool, tensor(a[1]), nullptr, k, v, {slots, starts, counts}, a[8], a[9], true);
+  const c10::cuda::CUDAGuard guard(pool.device());
+  check(unlocked(sa_cache_read, &r.c, (int32_t)integer(a[4]), r.B, r.T, ptr(k), ptr(v), rows_dtype(k), r.st.s,
+                 int_ptr(slots), int_ptr(starts), int_ptr(counts), stream()),
+        "sa_cache_read");
+  return tuple({pass(a[2]), pass(a[3])});
+}
+
+// cache_attend(pool, table, lens, q, layer, slots, counts, w, flags, scale, k_scale, v_scale, y, want_lse,
+//              lse, ws)
+PyObject* cache_attend(PyObject* const* a) {
+  const at::Tensor &pool = tensor(a[0]), &table = tensor(a[1]), &q = tensor(a[3]);
+  if (q.dim() != 4 || q.device() != pool.device())
+    raise(PyExc_ValueError, "q must be [B,Hq,T,d] on the cache's device");
+  sa_cache c = cache(&pool, table, &tensor(a[2]), nullptr, page_of(pool, q.size(3)), q.size(3));
+  c.k_scale = (float)real(a[10]);
+  c.v_scale = (float)real(a[11]);
+  const int dtype = rows_dtype(q);
+  const Strides qs = row_strides(q, false);
+  const at::Tensor *slots = tensor_or_null(a[5]), *counts = tensor_or_null(a[6]);
+  for (const at::Tensor* t : {slots, counts})
+    ints(t, {q.size(0)}, table, "slots and counts must be contiguous int32 [B] on the cache's device");
+  const int32_t B = (int32_t)q.size(0), Hq = (int32_t)q.size(1), T = (int32_t)q.size(2);
+  const at::Tensor *y_in = tensor_or_null(a[12]), *lse_in = tensor_or_null(a[14]);
+  if (y_in && (y_in->sizes() != q.sizes() || y_in->scalar_type() != q.scalar_type() || y_in->device() != q.device()))
+    raise(PyExc_ValueError, "y must have the shape and type of q");
+  if (lse_in && (lse_in->sizes() != q.sizes().slice(0, 3) || lse_in->scalar_type() != at::kFloat ||
+                 !lse_in->is_contiguous() || lse_in->device() != q.device()))
+    raise(PyExc_ValueError, "lse must be contiguous float32 [B,Hq,T]");
+  if (y_in) row_strides(*y_in, true);
+  const bool has_lse = lse_in || truth(a[13]);
+  const size_t need = sa_cache_attend_ws_bytes(&c, B, T, Hq, dtype);
+  size_t bytes;
+  void* ws;
+  const c10::cuda::OptionalCUDAGuard guard(pool.is_cuda() ? std::optional<c10::Device>(pool.device()) : std::nullopt);
+  const at::Tensor own = scratch(a[15], need, pool, "sa_cache_attend", &bytes, &ws);
+  Out y = output(a[12], [&] { return fresh(q.sizes(), q.scalar_type(), q.device()); });
+  const Strides ys = row_strides(y.t ? *y.t : y.own, true);
+  Out lse;
+  if (has_lse) lse = output(a[14], [&] { return rows_f32(q); });
+  check(unlocked(sa_cache_attend, &c, (int32_t)integer(a[4]), B, T, Hq, ptr(q), dtype, qs.s, int_ptr(slots),
+                 int_ptr(counts), (int32_t)integer(a[7]), (uint32_t)integer(a[8]), (float)real(a[9]), ptr(y), ys.s,
+                 has_lse ? (float*)ptr(lse) : nullptr, ws, bytes, stream()),
+        "sa_cache_attend");
+  return has_lse ? tuple({y.result(), lse.result()}) : y.result();
+}
+
+const at::Tensor& list_of(PyObject* o, const at::Tensor& table) {
+  const at::Tensor& t = tensor(o);
+  ints(&t, {t.numel()}, table, "slot lists must be contiguous int32 [n] on the cache's device");
+  return t;
+}
+
+// cache_free(table, lens, refs, slots)
+PyObject* cache_free(PyObject* const* a) {
+  const at::Tensor& table = tensor(a[0]);
+  const sa_cache c = cache(nullptr, table, &tensor(a[1]), &tensor(a[2]), 16, 16);
+  const at::Tensor& slots = list_of(a[3], table);
+  on_gpu(table);
+  const c10::cuda::CUDAGuard guard(table.device());
+  check(unlocked(sa_cache_free, &c, (int32_t)slots.numel(), int_ptr(&slots), stream()), "sa_cache_free");
+  return pass(Py_None);
+}
+
+// cache_fork(table, lens, refs, parents, children, page)
+PyObject* cache_fork(PyObject* const* a) {
+  const at::Tensor& table = tensor(a[0]);
+  const sa_cache c = cache(nullptr, table, &tensor(a[1]), &tensor(a[2]), integer(a[5]), 16);
+  const at::Tensor &parents = list_of(a[3], table), &children = list_of(a[4], table);
+  if (parents.numel() != children.numel())
+    raise(PyExc_ValueError, "parents and children must have one length");
+  on_gpu(table);
+  const c10::cuda::CUDAGuard guard(table.device());
+  check(unlocked(sa_cache_fork, &c, (int32_t)parents.numel(), int_ptr(&parents), int_ptr(&children), stream()),
+        "sa_cache_fork");
+  return pass(Py_None);
+}
+
+// The head dimension that a page of the pool has with this many tokens.
+int64_t head_dim(const at::Tensor& pool, int64_t page) {
+  return pool.dim() == 5 && page > 0 ? pool.size(4) * 16 / (9 * page) : 0;
+}
+
+// cache_reserve(pool, table, lens, refs, add, page, got, ws)
+PyObject* cache_reserve(PyObject* const* a) {
+  const at::Tensor &pool = tensor(a[0]), &table = tensor(a[1]), &add = tensor(a[4]);
+  const int64_t page = integer(a[5]);
+  const sa_cache c = cache(&pool, table, &tensor(a[2]), &tensor(a[3]), page, head_dim(pool, page));
+  ints(&add, {c.slots}, table, "add must be contiguous int32 [slots] on the cache's device");
+  ints(tensor_or_null(a[6]), {c.slots}, table, "got must be contiguous int32 [slots] on the cache's device");
+  size_t bytes;
+  void* ws;
+  const c10::cuda::OptionalCUDAGuard guard(pool.is_cuda() ? std::optional<c10::Device>(pool.device()) : std::nullopt);
+  const at::Tensor own = scratch(a[7], sa_cache_ws_bytes(&c), pool, "sa_cache_ws_bytes", &bytes, &ws);
+  Out got = output(a[6], [&] { return fresh({c.slots}, at::kInt, pool.device()); });
+  check(unlocked(sa_cache_reserve, &c, int_ptr(&add), (int32_t*)ptr(got), ws, bytes, stream()), "sa_cache_reserve");
+  return got.result();
+}
+
+// cache_compact(pool, table, refs, live, ws)
+PyObject* cache_compact(PyObject* const* a) {
+  const at::Tensor &pool = tensor(a[0]), &table = tensor(a[1]);
+  // any page and head dimension with the pool's bytes describe the moves
+  int64_t page = 128;
+  if (pool.dim() != 5) raise(PyExc_ValueError, "pool must be [layers, pages, Hkv, 2, bytes]");
+  while (page > 16 && (pool.size(4) % (9 * page) || head_dim(pool, page) < 16 || head_dim(pool, page) > 256)) page /= 2;
+  const sa_cache c = cache(&pool, table, nullptr, &tensor(a[2]), page, head_dim(pool, page));
+  ints(tensor_or_null(a[3]), {1}, table, "live must be int32 [1] on the cache's device");
+  size_t bytes;
+  void* ws;
+  const c10::cuda::OptionalCUDAGuard guard(pool.is_cuda() ? std::optional<c10::Device>(pool.device()) : std::nullopt);
+  const at::Tensor own = scratch(a[4], sa_cache_ws_bytes(&c), pool, "sa_cache_ws_bytes", &bytes, &ws);
+  Out live = output(a[3], [&] { return fresh({1}, at::kInt, pool.device()); });
+  check(unlocked(sa_cache_compact, &c, (int32_t*)ptr(live), ws, bytes, stream()), "sa_cache_compact");
+  return live.result();
+}
+
 template <PyObject* (*F)(PyObject* const*), int kArgs>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   if (nargs != kArgs) {
@@ -324,6 +570,13 @@ PyMethodDef g_methods[] = {
     SA_FAST(forward, 11),
     SA_FAST(gated_forward, 16),
     SA_FAST(backward, 19),
+    SA_FAST(cache_append, 10),
+    SA_FAST(cache_read, 10),
+    SA_FAST(cache_attend, 16),
+    SA_FAST(cache_free, 4),
+    SA_FAST(cache_fork, 6),
+    SA_FAST(cache_reserve, 8),
+    SA_FAST(cache_compact, 5),
     {"set_error_class", set_error_class, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
