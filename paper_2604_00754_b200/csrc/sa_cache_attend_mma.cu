@@ -16,21 +16,22 @@
 //   - The order of dimensions within a product is free: lane c of a quad takes the c-th quarter of a key's
 //     codes (one wide load), and Q's fragments are built to match.
 // Rounding.  Q is scaled per row by a power of two into fp16: exact for bf16 (8 bits) wherever it is within
-// 2^-31 of the row's largest; fp32 goes as two fp16 terms (22 bits and a remainder below 2^-24).  P, at most
-// 2^15 after the shift of the maximum (so that small ones stay normal in fp16), is rounded once to 11 bits
-// in bf16 calls, below the rounding of y, and goes as two terms in fp32 calls.  All sums are fp32.
+// 2^-31 of the row's largest; fp32 goes as two fp16 terms (22 bits and a remainder below 2^-24).  P is taken
+// relative to a reference that keeps it between 2^12 and 2^15.75 at its largest (small ones stay normal in
+// fp16, and the reference seldom moves); it is rounded once to 11 bits in bf16 calls, below the rounding of
+// y, and goes as two terms in fp32 calls.  All sums are fp32.
 #include "sa_cache_attend.cuh"
 
 namespace sa {
 using namespace attend;
 namespace {
 
-constexpr float kShift = 15.f;   // P is at most 2^15
+constexpr float kAim = 12.f, kMost = 15.75f;   // log2 of the largest P where the reference is set, and may be
+constexpr float kNone = -1e30f;                // reference before the first key
 
 template <int D>
-struct Tile {                    // a warp's ring slot: 16 keys
+struct Tile {                    // a warp's 16 keys
   static constexpr int kCodes = 8 * D, kScales = D, kBytes = 2 * (kCodes + kScales);
-  static constexpr int kStages = D == 64 ? 6 : D == 128 ? 4 : 3;
 };
 
 // Byte of 16-byte piece `piece` of a key's codes within a side's tile.  The pieces are permuted so that
@@ -99,35 +100,50 @@ struct Shape {
   static constexpr int kRows = 8 * NT;
   static constexpr int kKs = D / 16;                       // 16-deep steps of the scores, tiles of the sums
   static constexpr bool kQInRegs = kKs * 2 * NT * PC <= 32;
+  // Units a warp takes at once (one look at the maximum, one turn of the loop), as far as registers reach,
+  // and turns in its ring.
+  static constexpr int kUnits = D < 256 && NT == 1 ? 2 : 1;
+  static constexpr int kTurns = kUnits == 2 ? 3 : D == 64 ? 6 : D == 128 ? 4 : 3;
+  static constexpr int kRing = kTurns * kUnits * Tile<D>::kBytes;
   // CTAs per SM: what registers (rows of O, Q, the tile in flight) and shared memory leave
-  static constexpr int kCtas = kKs * 4 * NT + (kQInRegs ? kKs * 2 * NT * PC : 0) <= 48 ? 4
+  static constexpr int kCtas = kKs * 4 * NT + (kQInRegs ? kKs * 2 * NT * PC : 0) <= 40 ? 4
                                : kKs * 4 * NT <= 64 ? 3 : 2;
   static constexpr int kQBytes = kQInRegs ? 0 : kKs * NT * PC * 32 * 8;
   static constexpr int kOPitch = D + 4;
-  static constexpr int kOffQ = kWarps * Tile<D>::kStages * Tile<D>::kBytes;
+  static constexpr int kOffQ = kWarps * kRing;
   static constexpr int kOffO = kOffQ + kQBytes;            // [kRows][kOPitch] fp32
   static constexpr int kOffMl = kOffO + kRows * kOPitch * 4;   // [kWarps][2][kRows] fp32
-  static constexpr int kOffPages = kOffMl + kWarps * 2 * kRows * 4;   // [kWarps][64] int32
-  static constexpr int kSmem = kOffPages + kWarps * 64 * 4;
+  static constexpr int kOffPlaces = kOffMl + kWarps * 2 * kRows * 4;  // [kWarps][64] uint2
+  static constexpr int kSmem = kOffPlaces + kWarps * 64 * 8;
 };
 
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mma_kernel(const Params p) {
   using S = Shape<T, D, NT>;
-  constexpr int PC = S::PC, kRows = S::kRows, kKs = S::kKs, kStages = Tile<D>::kStages;
+  constexpr int PC = S::PC, kRows = S::kRows, kKs = S::kKs, U = S::kUnits, kTurns = S::kTurns;
   extern __shared__ __align__(128) uint8_t smem[];
   const AttendArgs& a = p.a;
   const CacheView& c = a.c;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int lr = lane >> 2, lc = lane & 3;                 // row and column of a lane in mma fragments
   const int key_k = (lr >> 1) + 4 * (lr & 1);              // key of this lane's row of S^T; the second is 8 on
-  uint8_t* ring = smem + warp * kStages * Tile<D>::kBytes;
+  uint8_t* ring = smem + warp * S::kRing;
   const uint32_t ring_u32 = (uint32_t)__cvta_generic_to_shared(ring);
   uint2* q_s = reinterpret_cast<uint2*>(smem + S::kOffQ);
   float* o_s = reinterpret_cast<float*>(smem + S::kOffO);
   float* ml_s = reinterpret_cast<float*>(smem + S::kOffMl);
-  int* pages = reinterpret_cast<int*>(smem + S::kOffPages) + warp * 64;
+  uint2* places = reinterpret_cast<uint2*>(smem + S::kOffPlaces) + warp * 64;
+  const uint32_t page_128 = (uint32_t)(c.page_bytes / 128);   // a page is a multiple of 1152 bytes from d = 64 on
   const int p_shift = 31 - __clz(c.P);
+
+  // where this lane reads in a unit's tile: K's rows key_k (8 on: 4 D bytes on), V's keys lc and lc + 4
+  const int at_k = D == 64 ? tile_at<D>(key_k, lc >> 1) + (lc & 1) * 8 : tile_at<D>(key_k, lc * (D / 128));
+  const int at_k1 = at_k ^ 16;             // the next piece (D = 256)
+  const int at_ks = 2 * Tile<D>::kCodes + key_k * (D / 16) + lc * (D / 64);
+  const int v_piece = D == 64 ? lr >> 2 : D == 128 ? lr >> 1 : lr, v_byte = D == 64 ? (lr & 3) * 4 : D == 128 ? (lr & 1) * 8 : 0;
+  const int at_v = Tile<D>::kCodes + tile_at<D>(lc, v_piece) + v_byte;
+  const int at_v4 = Tile<D>::kCodes + tile_at<D>(lc + 4, v_piece) + v_byte;
+  const int at_vs = 2 * Tile<D>::kCodes + Tile<D>::kScales + lc * (D / 16) + (D == 64 ? lr >> 1 : lr * (D / 128));
 
   grid_dependency_wait();
   grid_dependents_launch();
@@ -157,42 +173,57 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
     const int full_hi = a.causal ? min(en.len + t0 + 1, en.hi) : en.hi;   // (lengths and T are below 2^30)
     const int64_t full_lo = a.w > 0 ? (int64_t)en.len + t1 - a.w + 1 : 0;
 
-    // pages of units 0 .. 31 into the warp's list, of 32 .. 63 on the way
+    // places of units 0 .. 31 (K's codes in 128 bytes, K's scales in 64 bytes from the head's start of the
+    // pool; all ones: none) into the warp's list, of 32 .. 63 on the way
     const int32_t* table = c.table + (int64_t)en.slot * c.row;
-    auto fetch_page = [&](int i) -> int {
+    auto fetch_place = [&](int i) -> uint2 {
       const int64_t key = (int64_t)unit0 + (int64_t)i * kStep;
-      if (i >= units || key >= en.hi || key + kUnit <= en.lo) return -1;
-      const int pg = table[key >> p_shift];
-      if ((unsigned)pg < (unsigned)c.pages) return pg;
+      if (i >= units || key >= en.hi || key + kUnit <= en.lo) return make_uint2(~0u, ~0u);
+      const uint32_t pg = table[key >> p_shift];
+      if (pg < (uint32_t)c.pages) {
+        const uint32_t row = (uint32_t)key & (c.P - 1), at = pg * page_128;
+        return make_uint2(at + row * (D / 2) / 128, 2 * at + row * (D / 16) / 64);
+      }
       report_cache(c);
-      return -1;
+      return make_uint2(~0u, ~0u);
     };
     __syncwarp();
-    pages[lane] = fetch_page(lane);
-    int ahead = fetch_page(32 + lane);
+    places[lane] = fetch_place(lane);
+    uint2 ahead = fetch_place(32 + lane);
     __syncwarp();
 
-    auto issue = [&](int i) {
-      const int pg = i < units ? pages[i & 63] : -1;
-      if (pg >= 0) {
-        const int row = (unit0 + i * kStep) & (c.P - 1);
-        const uint8_t* src = cache_side(c, pg, h, 0) + row * (D / 2);
-        const uint32_t dst = ring_u32 + (i % kStages) * Tile<D>::kBytes;
+    // this lane's 16-byte pieces of a unit: D / 64 of K's codes and of V's, 512 bytes apart, and one of scales
+    const uint8_t* head = c.pool + (int64_t)2 * h * c.side;
+    const uint8_t *src_k = head + lane * 16, *src_v = src_k + c.side;
+    const uint8_t* src_s = head + c.P * (D / 2) + (lane < D / 16 ? 0 : c.side - D) + lane * 16;
+    const uint32_t dst_lane = ring_u32 + tile_at<D>(lane / (D / 32), lane % (D / 32));
+    const uint32_t dst_s = ring_u32 + 2 * Tile<D>::kCodes + lane * 16;
+    auto issue = [&](int turn, uint32_t slot) -> uint32_t {      // bits: units that are there
+      uint32_t there = 0;
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) {
-          const int x = lane + 32 * j, side = x / (D / 2), y = x % (D / 2);   // pieces of both sides' codes
-          copy16(dst + side * Tile<D>::kCodes + tile_at<D>(y / (D / 32), y % (D / 32)), src + side * c.side + y * 16);
-        }
-        if (lane < D / 8) {
-          const int side = lane / (D / 16), y = lane % (D / 16);
-          copy16(dst + 2 * Tile<D>::kCodes + lane * 16,
-                 cache_side(c, pg, h, side) + c.P * (D / 2) + row * (D / 16) + y * 16);
+      for (int u = 0; u < U; ++u) {
+        const int i = turn * U + u;
+        const uint2 at = places[i & 63];
+        if (i < units && at.x != ~0u) {
+          there |= 1u << u;
+          const uint32_t to = slot + u * Tile<D>::kBytes;
+          const uint8_t *k = src_k + (uint64_t)at.x * 128, *v = src_v + (uint64_t)at.x * 128;
+#pragma unroll
+          for (int j = 0; j < D / 64; ++j) {   // 32 pieces are 1024 / D keys: a multiple of 4, of 8 up to D = 128
+            const uint32_t x = D == 256 && (j & 1) ? (dst_lane ^ 16u) : dst_lane;
+            copy16(x + to + j * 512, k + j * 512);
+            copy16(x + to + Tile<D>::kCodes + j * 512, v + j * 512);
+          }
+          if (lane < D / 8) copy16(dst_s + to, src_s + (uint64_t)at.y * 64);
         }
       }
       copies_end();
+      return there;
     };
+    const int turns = (units + U - 1) / U;
+    uint32_t there = 0, slot = 0;              // of the last kTurns - 1 turns' units, the oldest on top
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) issue(i);
+    for (int i = 0; i < kTurns - 1; ++i) there = there << U | issue(i, i * U * Tile<D>::kBytes);
 
     // Q of this lane's fragments: row 8 nt + lr, the lc-th quarter of its dimensions
     uint32_t qf[S::kQInRegs ? NT : 1][PC][S::kQInRegs ? kKs : 1][2];
@@ -233,7 +264,8 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
       const int ex = (int)(top >> 23) - 127;
       const int up = ex == 128 || ex == -127 ? 0 : min(14 - ex, 126);
       const float by = __uint_as_float((uint32_t)(127 + up) << 23);
-      const float back = p.scale2 * __uint_as_float((uint32_t)(127 - up) << 23);
+      // not 0: a hidden score of -infinity stays one
+      const float back = fmaxf(p.scale2 * __uint_as_float((uint32_t)(127 - up) << 23), 1.2e-38f);
       factor[nt][0] = __shfl_sync(0xffffffffu, back, 8 * lc);
       factor[nt][1] = __shfl_sync(0xffffffffu, back, 8 * lc + 4);
 #pragma unroll
@@ -263,7 +295,7 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        m[nt][x] = -INFINITY;
+        m[nt][x] = kNone;
         l[nt][x] = 0.f;
       }
 #pragma unroll
@@ -271,43 +303,43 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) o[i][nt][0] = o[i][nt][1] = o[i][nt][2] = o[i][nt][3] = 0.f;
 
-    for (int i = 0; i < units; ++i) {
+    for (int turn = 0; turn < turns; ++turn) {
       __syncwarp();            // every lane has read the slot that the next copy fills
-      if ((i & 31) == 0 && i + 32 < units + kStages) {
-        pages[(i + 32 + lane) & 63] = ahead;
-        ahead = fetch_page(i + 64 + lane);
+      if ((turn & (32 / U - 1)) == 0) {
+        places[(turn * U + 32 + lane) & 63] = ahead;
+        ahead = fetch_place(turn * U + 64 + lane);
         __syncwarp();
       }
-      issue(i + kStages - 1);
-      copies_wait<kStages - 1>();
+      const uint32_t next = slot == 0 ? (kTurns - 1) * U * Tile<D>::kBytes : slot - U * Tile<D>::kBytes;
+      there = there << U | issue(turn + kTurns - 1, next);
+      copies_wait<kTurns - 1>();
       __syncwarp();
-      if (pages[i & 63] < 0) continue;
-      const uint8_t* tile = ring + (i % kStages) * Tile<D>::kBytes;
-      const uint8_t* k_scales = tile + 2 * Tile<D>::kCodes;
-      const uint8_t* v_scales = k_scales + Tile<D>::kScales;
-      const int unit = unit0 + i * kStep;
-      const bool full = unit + kUnit <= full_hi && unit >= full_lo;
+      const uint8_t* tiles = ring + slot;
+      slot = slot == (kTurns - 1) * U * Tile<D>::kBytes ? 0 : slot + U * Tile<D>::kBytes;
+      const uint32_t here = there >> (U * (kTurns - 1)) & ((1u << U) - 1u);
+      if (here == 0) continue;
+      const int unit = unit0 + turn * (U * kStep);
+      const bool full = here == (1u << U) - 1u && unit >= full_lo && unit + (U - 1) * kStep + kUnit <= full_hi;
 
       // scores of keys key_k, key_k + 8 (rows) and query rows 2 lc, 2 lc + 1 of each tile (columns)
-      float x[NT][4];
+      float x[U][NT][4];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) x[nt][0] = x[nt][1] = x[nt][2] = x[nt][3] = 0.f;
-      {
+      for (int un = 0; un < U; ++un) {
+        const uint8_t* tile = tiles + un * Tile<D>::kBytes;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) x[un][nt][0] = x[un][nt][1] = x[un][nt][2] = x[un][nt][3] = 0.f;
         constexpr int kWords = D / 32, kLoad = kWords < 4 ? kWords : 4;   // a lane's quarter of a key
         uint32_t w[2][kWords], sc[2][D == 256 ? 2 : 1];
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          const int key = key_k + 8 * z;
+        for (int z = 0; z < 2; ++z) {          // 8 keys on is 4 D bytes on, and the pieces lie alike
 #pragma unroll
           for (int u = 0; u < kWords / kLoad; ++u) {
             uint32_t v[kLoad];
-            const int at = D == 64 ? tile_at<D>(key, lc >> 1) + (lc & 1) * 8
-                                   : tile_at<D>(key, lc * (D / 128) + u);
-            load_words(v, tile + at);
+            load_words(v, tile + (u ? at_k1 : at_k) + z * 4 * D);
 #pragma unroll
             for (int y = 0; y < kLoad; ++y) w[z][u * kLoad + y] = v[y];
           }
-          const uint8_t* ks = k_scales + key * (D / 16) + lc * (D / 64);
+          const uint8_t* ks = tile + at_ks + z * (D / 2);
           if (D == 64) {
             sc[z][0] = scales_to_half2(*ks * 0x101u);
           } else if (D == 128) {
@@ -339,53 +371,60 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
               for (int z = PC - 1; z >= 0; --z) {
                 if (S::kQInRegs) {
                   const auto& f = qf[nt % (S::kQInRegs ? NT : 1)][z][ks % (S::kQInRegs ? kKs : 1)];
-                  mma(x[nt], fa, f[0], f[1]);
+                  mma(x[un][nt], fa, f[0], f[1]);
                 } else {
                   const uint2 f = q_s[((nt * PC + z) * kKs + ks) * 32 + lane];
-                  mma(x[nt], fa, f.x, f.y);
+                  mma(x[un][nt], fa, f.x, f.y);
                 }
               }
           }
         }
       }
+      // bit: key of the unit that some row sees; what the others have is whatever the page holds
+      uint32_t shown[U];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        x[nt][0] *= factor[nt][0];
-        x[nt][1] *= factor[nt][1];
-        x[nt][2] *= factor[nt][0];
-        x[nt][3] *= factor[nt][1];
-      }
-      // keys that no row sees have whatever the page holds
-      uint32_t shown = 0xffffu;        // bit: key of the unit that some row sees
+      for (int un = 0; un < U; ++un) shown[un] = 0xffffu;
       if (!full) {
-        shown &= 0xffffu << max(en.lo - unit, 0);
-        if (en.hi - unit < kUnit) shown &= (1u << (en.hi - unit)) - 1u;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int un = 0; un < U; ++un) {
+          const int first = unit + un * kStep;
+          const int below = min(max(en.lo - first, 0), kUnit), above = min(max(en.hi - first, 0), kUnit);
+          shown[un] = here >> un & 1 ? (1u << above) - (1u << min(below, above)) : 0u;
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const int r = 8 * nt + 2 * lc + (y & 1), key = key_k + (y & 2 ? 8 : 0);
-            const int pos = en.len + (en.r0 + r) / p.G, j = unit + key;
-            const bool sees = (shown >> key & 1) && (!a.causal || j <= pos) && (a.w <= 0 || pos - j < a.w);
-            if (!sees) x[nt][y] = -INFINITY;
-          }
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const int r = 8 * nt + 2 * lc + (y & 1), key = key_k + (y & 2 ? 8 : 0);
+              const int pos = en.len + (en.r0 + r) / p.G, j = first + key;
+              const bool sees = (shown[un] >> key & 1) && (!a.causal || j <= pos) && (a.w <= 0 || pos - j < a.w);
+              if (!sees) x[un][nt][y] = -INFINITY;
+            }
+        }
       }
-      // the running maximum: lanes look at each other only where one of them has more
+      // exponents relative to the reference m; lanes look at each other only where one has too much
       bool more = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
-        more |= x[nt][0] > m[nt][0] || x[nt][2] > m[nt][0] || x[nt][1] > m[nt][1] || x[nt][3] > m[nt][1];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int un = 0; un < U; ++un) top = fmaxf(top, fmaxf(x[un][nt][y], x[un][nt][y + 2]));
+          more |= fmaf(top, factor[nt][y], -m[nt][y]) > kMost;
+        }
       if (__any_sync(0xffffffffu, more)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            float top = fmaxf(x[nt][y], x[nt][y + 2]);
+            float top = -INFINITY;
+#pragma unroll
+            for (int un = 0; un < U; ++un) top = fmaxf(top, fmaxf(x[un][nt][y], x[un][nt][y + 2]));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-            const float to = fmaxf(m[nt][y], top);
-            const float keep = to == -INFINITY ? 1.f : exp2f(m[nt][y] - to);
+            const float to = fmaxf(m[nt][y], fmaf(top, factor[nt][y], -kAim));
+            const float keep = exp2f(m[nt][y] - to);
             m[nt][y] = to;
             l[nt][y] *= keep;
 #pragma unroll
@@ -395,44 +434,41 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
             }
           }
       }
-      uint32_t pf[NT][PC][2];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const float r0 = (m[nt][0] == -INFINITY ? 0.f : m[nt][0]) - kShift;
-        const float r1 = (m[nt][1] == -INFINITY ? 0.f : m[nt][1]) - kShift;
-        const float p0 = exp2f(x[nt][0] - r0), p1 = exp2f(x[nt][1] - r1);
-        const float p2 = exp2f(x[nt][2] - r0), p3 = exp2f(x[nt][3] - r1);
-        l[nt][0] += p0 + p2;
-        l[nt][1] += p1 + p3;
-        const uint32_t top = pack2(p0, p1), low = pack2(p2, p3);
-        pf[nt][0][0] = transpose8(top);
-        pf[nt][0][1] = transpose8(low);
-        if (PC == 2) {
-          pf[nt][PC - 1][0] = transpose8(rest2(p0, p1, top));
-          pf[nt][PC - 1][1] = transpose8(rest2(p2, p3, low));
+      for (int un = 0; un < U; ++un) {
+        const uint8_t* tile = tiles + un * Tile<D>::kBytes;
+        uint32_t pf[NT][PC][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float p0 = exp2f(fmaf(x[un][nt][0], factor[nt][0], -m[nt][0]));
+          const float p1 = exp2f(fmaf(x[un][nt][1], factor[nt][1], -m[nt][1]));
+          const float p2 = exp2f(fmaf(x[un][nt][2], factor[nt][0], -m[nt][0]));
+          const float p3 = exp2f(fmaf(x[un][nt][3], factor[nt][1], -m[nt][1]));
+          l[nt][0] += p0 + p2;
+          l[nt][1] += p1 + p3;
+          const uint32_t top = pack2(p0, p1), low = pack2(p2, p3);
+          pf[nt][0][0] = transpose8(top);
+          pf[nt][0][1] = transpose8(low);
+          if (PC == 2) {
+            pf[nt][PC - 1][0] = transpose8(rest2(p0, p1, top));
+            pf[nt][PC - 1][1] = transpose8(rest2(p2, p3, low));
+          }
         }
-      }
-
-      // sums: keys lc, lc + 4, lc + 8, lc + 12 and the lr-th eighth of the dimensions
-      {
+        // sums: keys lc, lc + 4, lc + 8, lc + 12 and the lr-th eighth of the dimensions
         constexpr int kWords = D / 64;
         uint32_t w[4][kWords], sv[4];           // words of a key; its scales, one byte or (D = 256) two
 #pragma unroll
         for (int z = 0; z < 4; ++z) {
-          const int key = lc + 4 * z;
-          const int at = D == 64 ? tile_at<D>(key, lr >> 2) + (lr & 3) * 4
-                         : D == 128 ? tile_at<D>(key, lr >> 1) + (lr & 1) * 8 : tile_at<D>(key, lr);
-          load_words(w[z], tile + Tile<D>::kCodes + at);
-          const uint8_t* vs = v_scales + key * (D / 16);
-          sv[z] = D == 64 ? vs[lr >> 1] : D == 128 ? vs[lr]
-                                                   : *reinterpret_cast<const uint16_t*>(vs + 2 * lr);
+          load_words(w[z], tile + (z & 1 ? at_v4 : at_v) + (z / 2) * 4 * D);
+          const uint8_t* vs = tile + at_vs + z * (D / 4);
+          sv[z] = D == 256 ? *reinterpret_cast<const uint16_t*>(vs) : *vs;
         }
         uint32_t poisoned[D == 256 ? 2 : 1] = {};     // bit: key whose values of this lane's group are NaN
         if (!full) {
           bool nan = false;
 #pragma unroll
           for (int z = 0; z < 4; ++z) {
-            if (!(shown >> (lc + 4 * z) & 1)) sv[z] = 0;
+            if (!(shown[un] >> (lc + 4 * z) & 1)) sv[z] = 0;
             nan |= (sv[z] & 0x7f) == 0x7f || (sv[z] & 0x7f00) == 0x7f00;
           }
           if (__any_sync(0xffffffffu, nan)) {
@@ -482,11 +518,11 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
-                  const int pos = en.len + (en.r0 + 8 * nt + 2 * lc + y) / p.G;
+                  const int pos = en.len + (en.r0 + 8 * nt + 2 * lc + y) / p.G, first = unit + un * kStep;
                   bool hit = false;
                   for (int key = 0; key < kUnit; ++key)
-                    hit |= (poisoned[g] >> key & 1) && (!a.causal || unit + key <= pos) &&
-                           (a.w <= 0 || pos - (unit + key) < a.w);
+                    hit |= (poisoned[g] >> key & 1) && (!a.causal || first + key <= pos) &&
+                           (a.w <= 0 || pos - (first + key) < a.w);
                   if (hit)
 #pragma unroll
                     for (int z = 0; z < kKs; ++z)
@@ -517,18 +553,14 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        const int r = 8 * nt + 2 * lc + y;
-        float to = -INFINITY;
+        float to = kNone;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) to = fmaxf(to, ml_s[w * 2 * kRows + r]);
-        const float keep = to == -INFINITY ? 0.f : exp2f(m[nt][y] - to);
+        for (int w = 0; w < kWarps; ++w) to = fmaxf(to, ml_s[w * 2 * kRows + 8 * nt + 2 * lc + y]);
+        const float keep = exp2f(m[nt][y] - to);
 #pragma unroll
         for (int z = 0; z < kKs; ++z) {
-          // a NaN stays one where no score counts
-          if (keep != 0.f || o[z][nt][y] != o[z][nt][y]) o[z][nt][y] *= keep;
-          else o[z][nt][y] = 0.f;
-          if (keep != 0.f || o[z][nt][y + 2] != o[z][nt][y + 2]) o[z][nt][y + 2] *= keep;
-          else o[z][nt][y + 2] = 0.f;
+          o[z][nt][y] *= keep;
+          o[z][nt][y + 2] *= keep;
         }
       }
     for (int w = 0; w < kWarps; ++w) {
@@ -556,24 +588,20 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
     if (!whole && k0 == 0) mine = Split{e, h, line.of(seg + en.n - 1) - (int)blockIdx.x + 1, 0};
     for (int i = tid; i < en.rows * D; i += 32 * kWarps) {
       const int r = i / D, x = i % D;
-      float to = -INFINITY;
+      float to = kNone, sum = 0.f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) to = fmaxf(to, ml_s[w * 2 * kRows + r]);
-      float sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float lw = ml_s[w * 2 * kRows + kRows + r];
-        const float keep = to == -INFINITY ? 1.f : exp2f(ml_s[w * 2 * kRows + r] - to);
-        sum += keep * lw;
-      }
+      for (int w = 0; w < kWarps; ++w)
+        sum += exp2f(ml_s[w * 2 * kRows + r] - to) * ml_s[w * 2 * kRows + kRows + r];
       const float v = o_s[r * S::kOPitch + (x % (D / 8)) / 2 * 16 + x / (D / 8) * 2 + (x & 1)];
       if (whole) {
         row_of(p, reinterpret_cast<T*>(a.y), a.ys, en, h, r)[x] = from_f32<T>(v * row_scale(sum, c.v_scale));
-        if (x == 0 && a.lse) *lse_of(p, en, h, r) = row_lse(to - kShift, sum);
+        if (x == 0 && a.lse) *lse_of(p, en, h, r) = row_lse(to, sum);
       } else {
         part[r * D + x] = v;
         if (x == 0) {
-          part[kRows * D + r] = to - kShift;      // as every part: the sum relative to the maximum
+          part[kRows * D + r] = to;
           part[kRows * (D + 1) + r] = sum;
         }
       }
