@@ -26,12 +26,12 @@ __global__ void __launch_bounds__(32 * kWarps) attend_kernel(const Params p) {
   int64_t before;
   const Line line = find(p, &e, &before);
   if (e < 0) {
-    if (tid == 0) p.split[blockIdx.x] = Split{0, 0, 0, 0};
+    if (!p.by_segment) file_split(p, 0, 0, 0);
     return;
   }
   int64_t s = line.begin(blockIdx.x);
   const int64_t end = line.begin(blockIdx.x + 1);
-  Split mine{0, 0, 0, 0};
+  bool begins = false;
   Entry en = entry(p, e);
   while (s < end) {
     while (en.n == 0 || s >= before + (int64_t)en.n * c.Hkv) {
@@ -150,7 +150,10 @@ __global__ void __launch_bounds__(32 * kWarps) attend_kernel(const Params p) {
     __syncthreads();
     const bool whole = k0 == 0 && k1 == en.n;
     float* part = part_of(p, blockIdx.x, k0 == 0);
-    if (!whole && k0 == 0) mine = Split{e, h, line.of(seg + en.n - 1) - (int)blockIdx.x + 1, 0};
+    if (k0 == 0) {
+      file_split(p, e, h, whole ? 1 : line.of(seg + en.n - 1) - (int)blockIdx.x + 1);
+      begins = true;
+    }
     for (int i = tid; i < en.rows * d; i += 32 * kWarps) {
       const int r = i / d, x = i - r * d;
       float to = -INFINITY;
@@ -177,57 +180,95 @@ __global__ void __launch_bounds__(32 * kWarps) attend_kernel(const Params p) {
     }
     s = seg + k1;
   }
-  if (tid == 0) p.split[blockIdx.x] = mine;
+  if (!begins && !p.by_segment) file_split(p, 0, 0, 0);
 }
 
-// Joins the parts of the segment that share blockIdx.x began: one row per blockIdx.y.
-template <typename T>
-__global__ void __launch_bounds__(32 * kWarps) join_kernel(const Params p) {
-  extern __shared__ float smem[];
+// Joins the parts of split segments.  A CTA has eight warps for rows / gridDim.y rows of one segment; the warps
+// of a row take every so-many-th part, each with a maximum of its own, and join in their order.  A part
+// is an L2 access away: four of them are on the way at once.
+constexpr int kJoinWarps = 8, kAtOnce = 4;
+
+template <typename T, int J>
+__global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const Params p) {
+  __shared__ float o_s[kJoinWarps][32 * J];
+  __shared__ float ml_s[kJoinWarps][2];
   const AttendArgs& a = p.a;
-  const int d = a.c.d, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = blockIdx.y;
+  const int d = a.c.d, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rows = p.rows;
   grid_dependency_wait();
-  const Split sp = p.split[blockIdx.x];
-  if (sp.parts == 0) return;
-  const Entry en = entry(p, sp.e);
-  if (r >= en.rows) return;
-  const int rows = p.rows;
-  auto part = [&](int i) { return part_of(p, blockIdx.x + i, i == 0); };
-  float to = -INFINITY;
-  for (int i = tid; i < sp.parts; i += 32 * kWarps) to = fmaxf(to, part(i)[rows * d + r]);
-  __shared__ float tops[kWarps];
-  to = warp_max(to);
-  if (lane == 0) tops[warp] = to;
-  __syncthreads();
+  const Split sp = p.split[blockIdx.x];                   // left over where nobody began the segment
+  const Entry en = entry(p, p.by_segment ? blockIdx.x / a.c.Hkv : sp.e);
+  if (en.n == 0 || sp.parts == 0) return;
+  const int mine = rows / gridDim.y, per = kJoinWarps / mine;   // rows of this CTA, warps of a row
+  const int r = blockIdx.y * mine + warp / per, sub = warp % per;
+  float m = -INFINITY, l = 0.f, o[J] = {};
+  if (r < en.rows) {
+    for (int i0 = sub; i0 < sp.parts; i0 += per * kAtOnce) {
+      float mi[kAtOnce], li[kAtOnce], v[kAtOnce][J];
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) to = fmaxf(to, tops[w]);
-  const float ref = to == -INFINITY ? 0.f : to;
-  // warp w adds up parts w, w + 4, ...; then the warps' sums in their order
-  float v[8] = {}, sum = 0.f;
-  for (int i = warp; i < sp.parts; i += kWarps) {
-    const float* f = part(i);
-    const float keep = exp2f(f[rows * d + r] - ref);
-    sum += keep * f[rows * (d + 1) + r];
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int i = i0 + k * per;
+        const bool there = i < sp.parts;
+        const float* f = part_of(p, sp.share + (there ? i : 0), !there || i == 0);
+        mi[k] = there ? f[rows * d + r] : -INFINITY;
+        li[k] = there ? f[rows * (d + 1) + r] : 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (lane + 32 * j < d) v[j] += keep * f[r * d + lane + 32 * j];
+        for (int j = 0; j < J; ++j) v[k][j] = there && lane + 32 * j < d ? f[r * d + lane + 32 * j] : 0.f;
+      }
+      float to = m;
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) to = fmaxf(to, mi[k]);
+      const float ref = to == -INFINITY ? 0.f : to, keep = exp2f(m - ref);
+      m = to;
+      l *= keep;
+#pragma unroll
+      for (int j = 0; j < J; ++j) o[j] *= keep;
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const float w = exp2f(mi[k] - ref);
+        l += w * li[k];
+#pragma unroll
+        for (int j = 0; j < J; ++j) o[j] += w * v[k][j];
+      }
+    }
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (lane + 32 * j < d) smem[warp * (d + 1) + lane + 32 * j] = v[j];
-  if (lane == 0) smem[warp * (d + 1) + d] = sum;
+  for (int j = 0; j < J; ++j) o_s[warp][lane + 32 * j] = o[j];
+  if (lane == 0) {
+    ml_s[warp][0] = m;
+    ml_s[warp][1] = l;
+  }
   __syncthreads();
-  sum = 0.f;
+  if (sub != 0 || r >= en.rows) return;
+  for (int k = 1; k < per; ++k) m = fmaxf(m, ml_s[warp + k][0]);
+  const float ref = m == -INFINITY ? 0.f : m;
+  l = 0.f;
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) sum += smem[w * (d + 1) + d];
+  for (int j = 0; j < J; ++j) o[j] = 0.f;
+  for (int k = 0; k < per; ++k) {
+    const float w = exp2f(ml_s[warp + k][0] - ref);
+    l += w * ml_s[warp + k][1];
+#pragma unroll
+    for (int j = 0; j < J; ++j) o[j] += w * o_s[warp + k][lane + 32 * j];
+  }
   T* y = row_of(p, reinterpret_cast<T*>(a.y), a.ys, en, sp.h, r);
-  for (int x = tid; x < d; x += 32 * kWarps) {
-    float o = 0.f;
+  const float by = row_scale(l, a.c.v_scale);
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) o += smem[w * (d + 1) + x];
-    y[x] = from_f32<T>(o * row_scale(sum, a.c.v_scale));
-  }
-  if (tid == 0 && a.lse) *lse_of(p, en, sp.h, r) = row_lse(to, sum);
+  for (int j = 0; j < J; ++j)
+    if (lane + 32 * j < d) y[lane + 32 * j] = from_f32<T>(o[j] * by);
+  if (lane == 0 && a.lse) *lse_of(p, en, sp.h, r) = row_lse(m, l);
+}
+
+template <typename T>
+cudaError_t join(const Params& p, cudaStream_t st) {
+  const int64_t segments = (int64_t)p.entries * p.a.c.Hkv;
+  // few segments have many parts each: a CTA per row, eight warps of which share the parts; many segments have
+  // two or three: a warp per row
+  const bool wide = segments * 8 < p.shares;
+  const dim3 grid((unsigned)(p.by_segment ? segments : p.shares), wide ? p.rows : p.rows / kJoinWarps);
+  const int d = p.a.c.d;
+  return d <= 64    ? launch_dependent(join_kernel<T, 2>, grid, dim3(32 * kJoinWarps), 0, st, p)
+         : d <= 128 ? launch_dependent(join_kernel<T, 4>, grid, dim3(32 * kJoinWarps), 0, st, p)
+                    : launch_dependent(join_kernel<T, 8>, grid, dim3(32 * kJoinWarps), 0, st, p);
 }
 
 template <typename T>
@@ -240,11 +281,8 @@ cudaError_t launch(const Params& p, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_cache_join(const Params& p, int dtype, cudaStream_t st) {
-  const dim3 grid(p.shares, p.rows);
-  const size_t smem = 4 * (size_t)kWarps * (p.a.c.d + 1);
   bump_launches();
-  return dtype == SA_BF16 ? launch_dependent(join_kernel<__nv_bfloat16>, grid, dim3(32 * kWarps), smem, st, p)
-                          : launch_dependent(join_kernel<float>, grid, dim3(32 * kWarps), smem, st, p);
+  return dtype == SA_BF16 ? join<__nv_bfloat16>(p, st) : join<float>(p, st);
 }
 
 static void shape(int T, int G, int d, int dtype, int* shares, int* rows) {

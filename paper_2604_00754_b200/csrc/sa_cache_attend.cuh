@@ -18,29 +18,32 @@ constexpr int kStep = 64;      // keys per step
 constexpr int kUnit = 16;      // keys a warp takes of a step; pages hold a multiple of it
 constexpr int kWarps = 4;
 
-// A split segment, filed under the share that begins it.
+// A split segment: the share that begins it and how many have a part of it (0: none is split).  Filed by
+// segment where the segments are no more than the shares, else by the share that begins it.
 struct Split {
-  int e, h, parts, pad;
+  int e, h, share, parts;
 };
 
 struct Params {
   AttendArgs a;
   int G, rows, tiles, entries;  // query heads per KV head, rows of a tile, tiles of a sequence, all entries
   int shares;                   // CTAs of the launch
+  bool by_segment;              // how splits are filed
+  bool few;                     // no line of steps that the table allows passes 31 bits
   float* part;                  // [shares][2][rows * (d + 2)]: a share's first and last segment
-  Split* split;                 // [shares]
+  Split* split;                 // [shares], or as many as there are segments
   float scale2;                 // scores times log2(e), K's power of two folded in
 };
 
 // Keys [lo, hi) that the rows of an entry may see, in steps [first, first + n); n = 0: no rows.
 struct Entry {
-  int b, slot, len, r0, rows, lo, hi, first, n;
+  int b, slot, len, r0, rows, t0, t1, lo, hi, first, n;   // t0 .. t1: the rows' tokens
 };
 
 __device__ inline Entry entry(const Params& p, int e) {
   const AttendArgs& a = p.a;
   Entry r{};
-  r.b = e / p.tiles;
+  r.b = p.tiles == 1 ? e : e / p.tiles;
   r.r0 = (e - r.b * p.tiles) * p.rows;
   const int count = cache_count(a.c, a.counts, r.b, a.T);
   if (count <= 0 || r.r0 >= p.G * count) return r;
@@ -53,73 +56,87 @@ __device__ inline Entry entry(const Params& p, int e) {
     return r;
   }
   r.rows = min(p.rows, p.G * count - r.r0);
-  const int t0 = r.r0 / p.G, t1 = (r.r0 + r.rows - 1) / p.G;
-  int64_t hi = a.causal ? (int64_t)r.len + t1 + 1 : r.len;
+  r.t0 = a.T == 1 ? 0 : r.r0 / p.G;
+  r.t1 = a.T == 1 ? 0 : (r.r0 + r.rows - 1) / p.G;
+  int64_t hi = a.causal ? (int64_t)r.len + r.t1 + 1 : r.len;
   if (hi > most) {
     report_cache(a.c);
     hi = most;
   }
   r.hi = (int)hi;
-  r.lo = a.w > 0 ? min((int)max((int64_t)r.len + t0 - a.w + 1, (int64_t)0), r.hi) : 0;
+  r.lo = a.w > 0 ? min((int)max((int64_t)r.len + r.t0 - a.w + 1, (int64_t)0), r.hi) : 0;
   r.first = r.lo / kStep;
   r.n = max((r.hi + kStep - 1) / kStep - r.first, 1);   // one step at least: empty rows are written too
   return r;
 }
 
-// Where the line of steps is cut: share i takes [total * i / shares, total * (i + 1) / shares).
+__device__ inline int64_t quotient(int64_t a, int64_t b) {   // of positive numbers, mostly small ones
+  return (a | b) >> 31 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
+// Where the line of steps is cut: every share takes `per` steps, the first `extra` one more.
 struct Line {
-  int64_t total;
-  int shares;
-  __device__ int64_t begin(int i) const { return total * i / shares; }
-  // the share that holds step s
-  __device__ int of(int64_t s) const { return (int)(((s + 1) * shares - 1) / total); }
+  int64_t total, per;
+  int shares, extra;
+  __device__ int64_t begin(int i) const { return i * per + min(i, extra); }
+  __device__ int of(int64_t s) const {      // the share that holds step s
+    const int64_t longer = extra * (per + 1);
+    return (int)(s < longer ? quotient(s, per + 1) : extra + quotient(s - longer, per));
+  }
 };
 
 // The line, and the entry that holds the first step of share `blockIdx.x` with the steps before that
 // entry.  Each thread adds up a run of entries; one scan of the runs' sums.  All threads call it.
-__device__ inline Line find(const Params& p, int* e_out, int64_t* before_out) {
-  __shared__ int64_t sums[kWarps];
-  __shared__ int64_t found_before;
+template <typename N>
+__device__ __forceinline__ Line find_in(const Params& p, int* e_out, int64_t* before_out) {
+  __shared__ N sums[kWarps];
+  __shared__ N found_before;
   __shared__ int found;
   const int tid = threadIdx.x, threads = 32 * kWarps;
-  const int run = (p.entries + threads - 1) / threads;
+  const int run = p.entries <= threads ? 1 : (p.entries + threads - 1) / threads;
   const int e0 = min(tid * run, p.entries), e1 = min(e0 + run, p.entries);
-  int64_t mine = 0;
+  N mine = 0;
   for (int e = e0; e < e1; ++e) mine += entry(p, e).n;
   mine *= p.a.c.Hkv;
-  int64_t upto = mine;
+  N upto = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int64_t v = __shfl_up_sync(0xffffffffu, upto, o);
+    const N v = __shfl_up_sync(0xffffffffu, upto, o);
     if ((tid & 31) >= o) upto += v;
   }
   if ((tid & 31) == 31) sums[tid >> 5] = upto;
   if (tid == 0) found = -1;
   __syncthreads();
-  Line line{0, 1};
+  Line line{};
   for (int i = 0; i < kWarps; ++i) {
     if (i < (tid >> 5)) upto += sums[i];
     line.total += sums[i];
   }
   line.shares = (int)min((int64_t)p.shares, line.total);
   if ((int)blockIdx.x < line.shares) {
-    const int64_t s = line.begin(blockIdx.x);
-    int64_t at = upto - mine;
-    if (s >= at && s < upto)
-      for (int e = e0; e < e1; ++e) {
-        const int64_t n = (int64_t)entry(p, e).n * p.a.c.Hkv;
-        if (s < at + n) {
-          found = e;
-          found_before = at;
-          break;
-        }
+    line.per = quotient(line.total, line.shares);
+    line.extra = (int)(line.total - line.per * line.shares);
+    const N s = (N)line.begin(blockIdx.x);
+    N at = upto - mine;
+    if (s >= at && s < upto) {
+      int e = e0;
+      while (run > 1) {
+        const N n = (N)entry(p, e).n * p.a.c.Hkv;
+        if (s < at + n) break;
         at += n;
+        ++e;
       }
+      found = e;
+      found_before = at;
+    }
   }
   __syncthreads();
   *e_out = found;
   *before_out = found_before;
   return line;
+}
+__device__ __forceinline__ Line find(const Params& p, int* e_out, int64_t* before_out) {
+  return p.few ? find_in<int32_t>(p, e_out, before_out) : find_in<int64_t>(p, e_out, before_out);
 }
 
 // One row of the result: o over its sum, and the log-sum-exp; m in log2 units, the sum relative to it.
@@ -140,6 +157,13 @@ __device__ __forceinline__ float* lse_of(const Params& p, const Entry& en, int h
   return p.a.lse + ((int64_t)en.b * p.a.Hq + h * p.G + g) * p.a.T + t;
 }
 
+// Files what became of a segment that this share begins.  Without `by_segment` a share's last one counts: of the
+// segments that it begins, only that can go on in the next.
+__device__ __forceinline__ void file_split(const Params& p, int e, int h, int parts) {
+  if (threadIdx.x == 0)
+    p.split[p.by_segment ? e * p.a.c.Hkv + h : (int)blockIdx.x] = Split{e, h, (int)blockIdx.x, parts > 1 ? parts : 0};
+}
+
 // Where a share's part of a segment goes: `last` where the share begins the segment.
 __device__ __forceinline__ float* part_of(const Params& p, int share, bool last) {
   return p.part + ((int64_t)share * 2 + last) * p.rows * (p.a.c.d + 2);
@@ -157,6 +181,8 @@ inline Params params(const AttendArgs& a, int shares, int rows) {
   p.tiles = (p.G * a.T + rows - 1) / rows;
   p.entries = a.B * p.tiles;
   p.shares = shares;
+  p.by_segment = (int64_t)p.entries * a.c.Hkv <= shares;
+  p.few = (double)p.entries * a.c.Hkv * ((double)a.c.row * a.c.P / kStep + 2) < 2e9;
   p.split = (Split*)a.ws;
   p.part = (float*)(p.split + shares);
   p.scale2 = a.scale * kLog2e * a.c.k_scale;

@@ -103,16 +103,17 @@ struct Shape {
   // Units a warp takes at once (one look at the maximum, one turn of the loop), as far as registers reach,
   // and turns in its ring.
   static constexpr int kUnits = D < 256 && NT == 1 ? 2 : 1;
-  static constexpr int kTurns = kUnits == 2 ? 3 : D == 64 ? 6 : D == 128 ? 4 : 3;
+  static constexpr int kTurns = kUnits == 2 ? (D == 64 ? 3 : 2) : D == 64 ? 6 : D == 128 ? 4 : 3;
   static constexpr int kRing = kTurns * kUnits * Tile<D>::kBytes;
   // CTAs per SM: what registers (rows of O, Q, the tile in flight) and shared memory leave
   static constexpr int kCtas = kKs * 4 * NT + (kQInRegs ? kKs * 2 * NT * PC : 0) <= 40 ? 4
                                : kKs * 4 * NT <= 64 ? 3 : 2;
   static constexpr int kQBytes = kQInRegs ? 0 : kKs * NT * PC * 32 * 8;
   static constexpr int kOPitch = D + 4;
+  static constexpr int kOs = NT == 1 && D <= 128 ? kWarps : 1;   // a warp's rows side by side, or one after the other
   static constexpr int kOffQ = kWarps * kRing;
-  static constexpr int kOffO = kOffQ + kQBytes;            // [kRows][kOPitch] fp32
-  static constexpr int kOffMl = kOffO + kRows * kOPitch * 4;   // [kWarps][2][kRows] fp32
+  static constexpr int kOffO = kOffQ + kQBytes;            // [kOs][kRows][kOPitch] fp32
+  static constexpr int kOffMl = kOffO + kOs * kRows * kOPitch * 4;   // [kWarps][2][kRows] fp32
   static constexpr int kOffPlaces = kOffMl + kWarps * 2 * kRows * 4;  // [kWarps][64] uint2
   static constexpr int kSmem = kOffPlaces + kWarps * 64 * 8;
 };
@@ -151,80 +152,96 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
   int64_t before;
   const Line line = find(p, &e, &before);
   if (e < 0) {
-    if (tid == 0) p.split[blockIdx.x] = Split{0, 0, 0, 0};
+    if (!p.by_segment) file_split(p, 0, 0, 0);
     return;
   }
   int64_t s = line.begin(blockIdx.x);
   const int64_t end = line.begin(blockIdx.x + 1);
-  Split mine{0, 0, 0, 0};
+  bool begins = false;
   Entry en = entry(p, e);
-  while (s < end) {
+  // the segment at hand: head, steps [k0, k1) of it, this warp's first unit (the next is kStep on)
+  int h, k0, k1, unit0, units, turns, full_hi;
+  int64_t seg, full_lo;
+  uint2 ahead;
+  const uint8_t *src_k, *src_v, *src_s;
+  uint32_t there, slot;      // units of the last kTurns - 1 turns, the oldest on top; ring slot of the next turn
+  const uint32_t dst_lane = ring_u32 + tile_at<D>(lane / (D / 32), lane % (D / 32));
+  const uint32_t dst_s = ring_u32 + 2 * Tile<D>::kCodes + lane * 16;
+
+  // places of units (K's codes in 128 bytes, K's scales in 64 bytes from the head's start of the pool; all
+  // ones: none)
+  auto fetch_place = [&](int i) -> uint2 {
+    const int64_t key = (int64_t)unit0 + (int64_t)i * kStep;
+    if (i >= units || key >= en.hi || key + kUnit <= en.lo) return make_uint2(~0u, ~0u);
+    const uint32_t pg = c.table[(int64_t)en.slot * c.row + (key >> p_shift)];
+    if (pg < (uint32_t)c.pages) {
+      const uint32_t row = (uint32_t)key & (c.P - 1), at = pg * page_128;
+      return make_uint2(at + row * (D / 2) / 128, 2 * at + row * (D / 16) / 64);
+    }
+    report_cache(c);
+    return make_uint2(~0u, ~0u);
+  };
+  auto issue = [&](int turn, uint32_t to_slot) -> uint32_t {      // bits: units that are there
+    uint32_t found = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = turn * U + u;
+      const uint2 at = places[i & 63];
+      if (i < units && at.x != ~0u) {
+        found |= 1u << u;
+        const uint32_t to = to_slot + u * Tile<D>::kBytes;
+        const uint8_t *k = src_k + (uint64_t)at.x * 128, *v = src_v + (uint64_t)at.x * 128;
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {   // 32 pieces are 1024 / D keys: a multiple of 4, of 8 up to D = 128
+          const uint32_t x = D == 256 && (j & 1) ? (dst_lane ^ 16u) : dst_lane;
+          copy16(x + to + j * 512, k + j * 512);
+          copy16(x + to + Tile<D>::kCodes + j * 512, v + j * 512);
+        }
+        if (lane < D / 8) copy16(dst_s + to, src_s + (uint64_t)at.y * 64);
+      }
+    }
+    copies_end();
+    return found;
+  };
+  // finds the segment at step s and starts its first copies; the warp has read what its ring held
+  auto open = [&] {
     while (en.n == 0 || s >= before + (int64_t)en.n * c.Hkv) {
       before += (int64_t)en.n * c.Hkv;
       en = entry(p, ++e);
     }
-    const int h = (int)((s - before) / en.n);
-    const int64_t seg = before + (int64_t)h * en.n;
-    const int k0 = (int)(s - seg), k1 = (int)min((int64_t)en.n, end - seg);
-    const int unit0 = (en.first + k0) * kStep + warp * kUnit;   // this warp's first unit; the next is kStep on
-    const int units = k1 - k0;
+    h = (int)quotient(s - before, en.n);
+    seg = before + (int64_t)h * en.n;
+    k0 = (int)(s - seg);
+    k1 = (int)min((int64_t)en.n, end - seg);
+    unit0 = (en.first + k0) * kStep + warp * kUnit;
+    units = k1 - k0;
+    turns = (units + U - 1) / U;
     // keys below full_hi and from full_lo on are seen by every row
-    const int t0 = en.r0 / p.G, t1 = (en.r0 + en.rows - 1) / p.G;
-    const int full_hi = a.causal ? min(en.len + t0 + 1, en.hi) : en.hi;   // (lengths and T are below 2^30)
-    const int64_t full_lo = a.w > 0 ? (int64_t)en.len + t1 - a.w + 1 : 0;
-
-    // places of units 0 .. 31 (K's codes in 128 bytes, K's scales in 64 bytes from the head's start of the
-    // pool; all ones: none) into the warp's list, of 32 .. 63 on the way
-    const int32_t* table = c.table + (int64_t)en.slot * c.row;
-    auto fetch_place = [&](int i) -> uint2 {
-      const int64_t key = (int64_t)unit0 + (int64_t)i * kStep;
-      if (i >= units || key >= en.hi || key + kUnit <= en.lo) return make_uint2(~0u, ~0u);
-      const uint32_t pg = table[key >> p_shift];
-      if (pg < (uint32_t)c.pages) {
-        const uint32_t row = (uint32_t)key & (c.P - 1), at = pg * page_128;
-        return make_uint2(at + row * (D / 2) / 128, 2 * at + row * (D / 16) / 64);
-      }
-      report_cache(c);
-      return make_uint2(~0u, ~0u);
-    };
-    __syncwarp();
-    places[lane] = fetch_place(lane);
-    uint2 ahead = fetch_place(32 + lane);
-    __syncwarp();
-
+    full_hi = a.causal ? min(en.len + en.t0 + 1, en.hi) : en.hi;   // (lengths and T are below 2^30)
+    full_lo = a.w > 0 ? (int64_t)en.len + en.t1 - a.w + 1 : 0;
+    // rows of Q on their way while the places are looked up
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+      if (8 * nt + lr < en.rows)
+        asm volatile("prefetch.global.L1 [%0];" ::"l"(row_of(p, reinterpret_cast<const T*>(a.q), a.qs, en, h, 8 * nt + lr) +
+                                                     lc * (D / 4)));
     // this lane's 16-byte pieces of a unit: D / 64 of K's codes and of V's, 512 bytes apart, and one of scales
     const uint8_t* head = c.pool + (int64_t)2 * h * c.side;
-    const uint8_t *src_k = head + lane * 16, *src_v = src_k + c.side;
-    const uint8_t* src_s = head + c.P * (D / 2) + (lane < D / 16 ? 0 : c.side - D) + lane * 16;
-    const uint32_t dst_lane = ring_u32 + tile_at<D>(lane / (D / 32), lane % (D / 32));
-    const uint32_t dst_s = ring_u32 + 2 * Tile<D>::kCodes + lane * 16;
-    auto issue = [&](int turn, uint32_t slot) -> uint32_t {      // bits: units that are there
-      uint32_t there = 0;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = turn * U + u;
-        const uint2 at = places[i & 63];
-        if (i < units && at.x != ~0u) {
-          there |= 1u << u;
-          const uint32_t to = slot + u * Tile<D>::kBytes;
-          const uint8_t *k = src_k + (uint64_t)at.x * 128, *v = src_v + (uint64_t)at.x * 128;
-#pragma unroll
-          for (int j = 0; j < D / 64; ++j) {   // 32 pieces are 1024 / D keys: a multiple of 4, of 8 up to D = 128
-            const uint32_t x = D == 256 && (j & 1) ? (dst_lane ^ 16u) : dst_lane;
-            copy16(x + to + j * 512, k + j * 512);
-            copy16(x + to + Tile<D>::kCodes + j * 512, v + j * 512);
-          }
-          if (lane < D / 8) copy16(dst_s + to, src_s + (uint64_t)at.y * 64);
-        }
-      }
-      copies_end();
-      return there;
-    };
-    const int turns = (units + U - 1) / U;
-    uint32_t there = 0, slot = 0;              // of the last kTurns - 1 turns' units, the oldest on top
+    src_k = head + lane * 16;
+    src_v = src_k + c.side;
+    src_s = head + c.P * (D / 2) + (lane < D / 16 ? 0 : c.side - D) + lane * 16;
+    // places of units 0 .. 31 into the warp's list, of 32 .. 63 on the way
+    __syncwarp();
+    places[lane] = fetch_place(lane);
+    ahead = fetch_place(32 + lane);
+    __syncwarp();
+    there = slot = 0;
 #pragma unroll
     for (int i = 0; i < kTurns - 1; ++i) there = there << U | issue(i, i * U * Tile<D>::kBytes);
+  };
 
+  open();
+  for (;;) {
     // Q of this lane's fragments: row 8 nt + lr, the lc-th quarter of its dimensions
     uint32_t qf[S::kQInRegs ? NT : 1][PC][S::kQInRegs ? kKs : 1][2];
     float factor[NT][2];      // log2 units per unit of a score, of the two columns 2 lc, 2 lc + 1
@@ -531,7 +548,17 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
         }
       }
     }
-    copies_wait<0>();
+    // the next segment's copies start before this one is joined
+    const Entry done = en;
+    const int done_h = h, done_k0 = k0;
+    const bool whole = k0 == 0 && k1 == en.n;
+    if (k0 == 0) {
+      file_split(p, e, h, whole ? 1 : line.of(seg + en.n - 1) - (int)blockIdx.x + 1);
+      begins = true;
+    }
+    s = seg + k1;
+    __syncwarp();
+    if (s < end) open();
 
     // the warps join: maximum and sums first, then the rows, one warp after the other
     __syncthreads();           // o_s of the last segment has been read
@@ -563,8 +590,9 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
           o[z][nt][y + 2] *= keep;
         }
       }
-    for (int w = 0; w < kWarps; ++w) {
-      if (warp == w) {
+    for (int w = 0; w < (S::kOs == 1 ? kWarps : 1); ++w) {
+      if (S::kOs > 1 || warp == w) {
+        float* mine = o_s + (S::kOs > 1 ? warp * kRows * S::kOPitch : 0);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -572,7 +600,7 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
 #pragma unroll
             for (int z = 0; z < kKs; ++z) {
               // dimension lr * D / 8 + 2 z and the next: side by side, eighths next to each other
-              float2* at = reinterpret_cast<float2*>(o_s + (8 * nt + 2 * lc + y) * S::kOPitch + 16 * z + 2 * lr);
+              float2* at = reinterpret_cast<float2*>(mine + (8 * nt + 2 * lc + y) * S::kOPitch + 16 * z + 2 * lr);
               float2 v = make_float2(o[z][nt][y], o[z][nt][y + 2]);
               if (w) {
                 v.x += at->x;
@@ -583,10 +611,8 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
       }
       __syncthreads();
     }
-    const bool whole = k0 == 0 && k1 == en.n;
-    float* part = part_of(p, blockIdx.x, k0 == 0);
-    if (!whole && k0 == 0) mine = Split{e, h, line.of(seg + en.n - 1) - (int)blockIdx.x + 1, 0};
-    for (int i = tid; i < en.rows * D; i += 32 * kWarps) {
+    float* part = part_of(p, blockIdx.x, done_k0 == 0);
+    for (int i = tid; i < done.rows * D; i += 32 * kWarps) {
       const int r = i / D, x = i % D;
       float to = kNone, sum = 0.f;
 #pragma unroll
@@ -594,10 +620,13 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
 #pragma unroll
       for (int w = 0; w < kWarps; ++w)
         sum += exp2f(ml_s[w * 2 * kRows + r] - to) * ml_s[w * 2 * kRows + kRows + r];
-      const float v = o_s[r * S::kOPitch + (x % (D / 8)) / 2 * 16 + x / (D / 8) * 2 + (x & 1)];
+      float v = 0.f;
+#pragma unroll
+      for (int w = 0; w < S::kOs; ++w)
+        v += o_s[(w * kRows + r) * S::kOPitch + (x % (D / 8)) / 2 * 16 + x / (D / 8) * 2 + (x & 1)];
       if (whole) {
-        row_of(p, reinterpret_cast<T*>(a.y), a.ys, en, h, r)[x] = from_f32<T>(v * row_scale(sum, c.v_scale));
-        if (x == 0 && a.lse) *lse_of(p, en, h, r) = row_lse(to, sum);
+        row_of(p, reinterpret_cast<T*>(a.y), a.ys, done, done_h, r)[x] = from_f32<T>(v * row_scale(sum, c.v_scale));
+        if (x == 0 && a.lse) *lse_of(p, done, done_h, r) = row_lse(to, sum);
       } else {
         part[r * D + x] = v;
         if (x == 0) {
@@ -606,9 +635,9 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
         }
       }
     }
-    s = seg + k1;
+    if (s >= end) break;
   }
-  if (tid == 0) p.split[blockIdx.x] = mine;
+  if (!begins && !p.by_segment) file_split(p, 0, 0, 0);
 }
 
 template <typename T, int D, int NT>
