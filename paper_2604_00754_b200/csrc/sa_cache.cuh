@@ -16,7 +16,7 @@ namespace sa {
 struct CacheView {
   uint8_t* pool;
   const int32_t *table, *lens;
-  int pages, Hkv, d, P, slots, row;
+  int pages, Hkv, d, P, p_shift, slots, row;   // P = 1 << p_shift
   int side;               // bytes of one head and side of a page
   int64_t page_bytes;     // of one layer
   float k_scale, v_scale;
@@ -49,7 +49,7 @@ __device__ __forceinline__ int cache_count(const CacheView& c, const int32_t* co
 
 // Page that holds token `pos` (not negative) of a slot, or -1 (reported) where the slot has none there.
 __device__ __forceinline__ int cache_page(const CacheView& c, int slot, int64_t pos) {
-  const int64_t i = pos / c.P;
+  const int64_t i = pos >> c.p_shift;
   if (i < c.row) {
     const int p = c.table[(int64_t)slot * c.row + i];
     if ((unsigned)p < (unsigned)c.pages) return p;

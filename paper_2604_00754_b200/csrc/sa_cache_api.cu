@@ -20,7 +20,7 @@ sa_status check_geometry(const sa_cache* c) {
   if (c->layers < 1 || c->pages < 1 || c->Hkv < 1 || c->d < 1 || c->slots < 1 || c->row < 1)
     return SA_ERR_INVALID_ARG;
   if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return SA_ERR_INVALID_ARG;
-  if (c->d % 16 != 0 || c->d > 256 || c->Hkv > 65535) return SA_ERR_UNSUPPORTED;
+  if (c->d % 16 != 0 || c->d > 256 || c->Hkv > 32767) return SA_ERR_UNSUPPORTED;
   // positions are 32-bit
   if ((int64_t)c->row * c->page > (1ll << 30)) return SA_ERR_UNSUPPORTED;
   return SA_OK;
@@ -65,6 +65,7 @@ CacheView view(const sa_cache* c, int32_t layer, int* status) {
   v.Hkv = c->Hkv;
   v.d = c->d;
   v.P = c->page;
+  v.p_shift = c->page == 16 ? 4 : c->page == 32 ? 5 : c->page == 64 ? 6 : 7;
   v.slots = c->slots;
   v.row = c->row;
   v.side = c->page * (c->d / 2 + c->d / 16);
@@ -82,8 +83,6 @@ sa_status rows(const sa_cache* c, bool read, int32_t layer, int32_t B, int32_t T
   if (!k || !v || !aligned(k, 16) || !aligned(v, 16) || !good_strides(stride, c->d, T) ||
       !ints_or_null(slots) || !ints_or_null(starts) || !ints_or_null(counts))
     return SA_ERR_INVALID_ARG;
-  // groups of 16 dimensions of a sequence are counted in 32 bits
-  if ((int64_t)T * c->Hkv * 2 * (c->d / 16) > 0xffffff00ll) return SA_ERR_UNSUPPORTED;
   int* status = cache_status_ptr();
   if (!status) return SA_ERR_CUDA;
   return launch_cache_rows(view(c, layer, status), read, B, T, k, v, dtype, stride, slots, starts, counts,

@@ -135,7 +135,6 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
   float* ml_s = reinterpret_cast<float*>(smem + S::kOffMl);
   uint2* places = reinterpret_cast<uint2*>(smem + S::kOffPlaces) + warp * 64;
   const uint32_t page_128 = (uint32_t)(c.page_bytes / 128);   // a page is a multiple of 1152 bytes from d = 64 on
-  const int p_shift = 31 - __clz(c.P);
 
   // where this lane reads in a unit's tile: K's rows key_k (8 on: 4 D bytes on), V's keys lc and lc + 4
   const int at_k = D == 64 ? tile_at<D>(key_k, lc >> 1) + (lc & 1) * 8 : tile_at<D>(key_k, lc * (D / 128));
@@ -173,7 +172,7 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
   auto fetch_place = [&](int i) -> uint2 {
     const int64_t key = (int64_t)unit0 + (int64_t)i * kStep;
     if (i >= units || key >= en.hi || key + kUnit <= en.lo) return make_uint2(~0u, ~0u);
-    const uint32_t pg = c.table[(int64_t)en.slot * c.row + (key >> p_shift)];
+    const uint32_t pg = c.table[(int64_t)en.slot * c.row + (key >> c.p_shift)];
     if (pg < (uint32_t)c.pages) {
       const uint32_t row = (uint32_t)key & (c.P - 1), at = pg * page_128;
       return make_uint2(at + row * (D / 2) / 128, 2 * at + row * (D / 16) / 64);
