@@ -20,6 +20,8 @@
 // relative to a reference that keeps it between 2^12 and 2^15.75 at its largest (small ones stay normal in
 // fp16, and the reference seldom moves); it is rounded once to 11 bits in bf16 calls, below the rounding of
 // y, and goes as two terms in fp32 calls.  All sums are fp32.
+#include <type_traits>
+
 #include "sa_cache_attend.cuh"
 
 namespace sa {
@@ -99,15 +101,19 @@ struct Shape {
   static constexpr int PC = sizeof(T) == 2 ? 1 : 2;
   static constexpr int kRows = 8 * NT;
   static constexpr int kKs = D / 16;                       // 16-deep steps of the scores, tiles of the sums
-  static constexpr bool kQInRegs = kKs * 2 * NT * PC <= 32;
+  static constexpr bool kQInRegs = kKs * 2 * NT * PC <= (NT == 1 && D < 256 ? 32 : 16);   // else in shared memory
   // Units a warp takes at once (one look at the maximum, one turn of the loop), as far as registers reach,
   // and turns in its ring.
   static constexpr int kUnits = D < 256 && NT == 1 ? 2 : 1;
   static constexpr int kTurns = kUnits == 2 ? (D == 64 ? 3 : 2) : D == 64 ? 6 : D == 128 ? 4 : 3;
   static constexpr int kRing = kTurns * kUnits * Tile<D>::kBytes;
-  // CTAs per SM: what registers (rows of O, Q, the tile in flight) and shared memory leave
-  static constexpr int kCtas = kKs * 4 * NT + (kQInRegs ? kKs * 2 * NT * PC : 0) <= 40 ? 4
-                               : kKs * 4 * NT <= 64 ? 3 : 2;
+  // CTAs per SM: what registers (rows of O, Q, the tile in flight) and shared memory leave.  64 registers of O:
+  // two CTAs without spills beat three with them in one tile of rows and in four (16 x 8192 keys, 16/4 heads of 256
+  // 45.9 against 46.8 us, 37 fp32 rows over 2500 keys of 16 heads of 64 64.8 against 70.7), not in two (four
+  // tokens over 16 x 8192 keys, 32/8 heads of 128: 67.1 against 64.2).
+  static constexpr int kORegs = kKs * 4 * NT;
+  static constexpr int kCtas = kORegs + (kQInRegs ? kKs * 2 * NT * PC : 0) <= 40 ? 4
+                               : kORegs < 64 || (kORegs == 64 && NT == 2) ? 3 : 2;
   static constexpr int kQBytes = kQInRegs ? 0 : kKs * NT * PC * 32 * 8;
   static constexpr int kOPitch = D + 4;
   static constexpr int kOs = NT == 1 && D <= 128 ? kWarps : 1;   // a warp's rows side by side, or one after the other
@@ -336,99 +342,91 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
       if (here == 0) continue;
       const int unit = unit0 + turn * (U * kStep);
       const bool full = here == (1u << U) - 1u && unit >= full_lo && unit + (U - 1) * kStep + kUnit <= full_hi;
-
-      // scores of keys key_k, key_k + 8 (rows) and query rows 2 lc, 2 lc + 1 of each tile (columns)
-      float x[U][NT][4];
+      // two copies of the code: where every row sees every key, no branch stands between what can overlap
+      auto take = [&](auto seen_by_all) {
+        constexpr bool kFull = decltype(seen_by_all)::value;
+        // scores of keys key_k, key_k + 8 (rows) and query rows 2 lc, 2 lc + 1 of each tile (columns)
+        float x[U][NT][4];
 #pragma unroll
-      for (int un = 0; un < U; ++un) {
-        const uint8_t* tile = tiles + un * Tile<D>::kBytes;
+        for (int un = 0; un < U; ++un) {
+          const uint8_t* tile = tiles + un * Tile<D>::kBytes;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) x[un][nt][0] = x[un][nt][1] = x[un][nt][2] = x[un][nt][3] = 0.f;
-        constexpr int kWords = D / 32, kLoad = kWords < 4 ? kWords : 4;   // a lane's quarter of a key
-        uint32_t w[2][kWords], sc[2][D == 256 ? 2 : 1];
+          for (int nt = 0; nt < NT; ++nt) x[un][nt][0] = x[un][nt][1] = x[un][nt][2] = x[un][nt][3] = 0.f;
+          constexpr int kWords = D / 32, kLoad = kWords < 4 ? kWords : 4;   // a lane's quarter of a key
+          uint32_t w[2][kWords], sc[2][D == 256 ? 2 : 1];
 #pragma unroll
-        for (int z = 0; z < 2; ++z) {          // 8 keys on is 4 D bytes on, and the pieces lie alike
+          for (int z = 0; z < 2; ++z) {          // 8 keys on is 4 D bytes on, and the pieces lie alike
 #pragma unroll
-          for (int u = 0; u < kWords / kLoad; ++u) {
-            uint32_t v[kLoad];
-            load_words(v, tile + (u ? at_k1 : at_k) + z * 4 * D);
+            for (int u = 0; u < kWords / kLoad; ++u) {
+              uint32_t v[kLoad];
+              load_words(v, tile + (u ? at_k1 : at_k) + z * 4 * D);
 #pragma unroll
-            for (int y = 0; y < kLoad; ++y) w[z][u * kLoad + y] = v[y];
+              for (int y = 0; y < kLoad; ++y) w[z][u * kLoad + y] = v[y];
+            }
+            const uint8_t* ks = tile + at_ks + z * (D / 2);
+            if (D == 64) {
+              sc[z][0] = scales_to_half2(*ks * 0x101u);
+            } else if (D == 128) {
+              sc[z][0] = scales_to_half2(*reinterpret_cast<const uint16_t*>(ks));
+            } else {
+              const uint32_t four = *reinterpret_cast<const uint32_t*>(ks);
+              sc[z][0] = scales_to_half2(four);
+              sc[z][D == 256 ? 1 : 0] = scales_to_half2(four >> 16);
+            }
           }
-          const uint8_t* ks = tile + at_ks + z * (D / 2);
-          if (D == 64) {
-            sc[z][0] = scales_to_half2(*ks * 0x101u);
-          } else if (D == 128) {
-            sc[z][0] = scales_to_half2(*reinterpret_cast<const uint16_t*>(ks));
-          } else {
-            const uint32_t four = *reinterpret_cast<const uint32_t*>(ks);
-            sc[z][0] = scales_to_half2(four);
-            sc[z][D == 256 ? 1 : 0] = scales_to_half2(four >> 16);
+#pragma unroll
+          for (int u = 0; u < kWords; ++u) {      // eight dimensions of this lane: two 16-deep steps
+            uint32_t v[2][4];
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+              codes_to_half2(w[z][u], v[z]);
+              const int g = u / 2;                // its group of 16
+              const uint32_t two = D == 64 ? sc[z][0] : __byte_perm(sc[z][D == 256 ? g / 2 : 0], 0, g & 1 ? 0x3232 : 0x1010);
+#pragma unroll
+              for (int y = 0; y < 4; ++y) v[z][y] = mul2(v[z][y], two);
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              const uint32_t fa[4] = {v[0][2 * y], v[1][2 * y], v[0][2 * y + 1], v[1][2 * y + 1]};
+              const int ks = 2 * u + y;
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int z = PC - 1; z >= 0; --z) {
+                  if (S::kQInRegs) {
+                    const auto& f = qf[nt % (S::kQInRegs ? NT : 1)][z][ks % (S::kQInRegs ? kKs : 1)];
+                    mma(x[un][nt], fa, f[0], f[1]);
+                  } else {
+                    const uint2 f = q_s[((nt * PC + z) * kKs + ks) * 32 + lane];
+                    mma(x[un][nt], fa, f.x, f.y);
+                  }
+                }
+            }
           }
         }
+        // bit: key of the unit that some row sees; what the others have is whatever the page holds
+        uint32_t shown[U];
 #pragma unroll
-        for (int u = 0; u < kWords; ++u) {      // eight dimensions of this lane: two 16-deep steps
-          uint32_t v[2][4];
+        for (int un = 0; un < U; ++un) shown[un] = 0xffffu;
+        if (!kFull) {
 #pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            codes_to_half2(w[z][u], v[z]);
-            const int g = u / 2;                // its group of 16
-            const uint32_t two = D == 64 ? sc[z][0] : __byte_perm(sc[z][D == 256 ? g / 2 : 0], 0, g & 1 ? 0x3232 : 0x1010);
-#pragma unroll
-            for (int y = 0; y < 4; ++y) v[z][y] = mul2(v[z][y], two);
-          }
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const uint32_t fa[4] = {v[0][2 * y], v[1][2 * y], v[0][2 * y + 1], v[1][2 * y + 1]};
-            const int ks = 2 * u + y;
+          for (int un = 0; un < U; ++un) {
+            const int first = unit + un * kStep;
+            const int below = min(max(en.lo - first, 0), kUnit), above = min(max(en.hi - first, 0), kUnit);
+            shown[un] = here >> un & 1 ? (1u << above) - (1u << min(below, above)) : 0u;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int z = PC - 1; z >= 0; --z) {
-                if (S::kQInRegs) {
-                  const auto& f = qf[nt % (S::kQInRegs ? NT : 1)][z][ks % (S::kQInRegs ? kKs : 1)];
-                  mma(x[un][nt], fa, f[0], f[1]);
-                } else {
-                  const uint2 f = q_s[((nt * PC + z) * kKs + ks) * 32 + lane];
-                  mma(x[un][nt], fa, f.x, f.y);
-                }
+              for (int y = 0; y < 4; ++y) {
+                const int r = 8 * nt + 2 * lc + (y & 1), key = key_k + (y & 2 ? 8 : 0);
+                const int pos = en.len + (en.r0 + r) / p.G, j = first + key;
+                const bool sees = (shown[un] >> key & 1) && (!a.causal || j <= pos) && (a.w <= 0 || pos - j < a.w);
+                if (!sees) x[un][nt][y] = -INFINITY;
               }
           }
         }
-      }
-      // bit: key of the unit that some row sees; what the others have is whatever the page holds
-      uint32_t shown[U];
-#pragma unroll
-      for (int un = 0; un < U; ++un) shown[un] = 0xffffu;
-      if (!full) {
-#pragma unroll
-        for (int un = 0; un < U; ++un) {
-          const int first = unit + un * kStep;
-          const int below = min(max(en.lo - first, 0), kUnit), above = min(max(en.hi - first, 0), kUnit);
-          shown[un] = here >> un & 1 ? (1u << above) - (1u << min(below, above)) : 0u;
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              const int r = 8 * nt + 2 * lc + (y & 1), key = key_k + (y & 2 ? 8 : 0);
-              const int pos = en.len + (en.r0 + r) / p.G, j = first + key;
-              const bool sees = (shown[un] >> key & 1) && (!a.causal || j <= pos) && (a.w <= 0 || pos - j < a.w);
-              if (!sees) x[un][nt][y] = -INFINITY;
-            }
-        }
-      }
-      // exponents relative to the reference m; lanes look at each other only where one has too much
-      bool more = false;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          float top = -INFINITY;
-#pragma unroll
-          for (int un = 0; un < U; ++un) top = fmaxf(top, fmaxf(x[un][nt][y], x[un][nt][y + 2]));
-          more |= fmaf(top, factor[nt][y], -m[nt][y]) > kMost;
-        }
-      if (__any_sync(0xffffffffu, more)) {
+        // exponents relative to the reference m; lanes look at each other only where one has too much
+        bool more = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -436,117 +434,131 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
             float top = -INFINITY;
 #pragma unroll
             for (int un = 0; un < U; ++un) top = fmaxf(top, fmaxf(x[un][nt][y], x[un][nt][y + 2]));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-            const float to = fmaxf(m[nt][y], fmaf(top, factor[nt][y], -kAim));
-            const float keep = exp2f(m[nt][y] - to);
-            m[nt][y] = to;
-            l[nt][y] *= keep;
+            more |= fmaf(top, factor[nt][y], -m[nt][y]) > kMost;
+          }
+        if (__any_sync(0xffffffffu, more)) {
 #pragma unroll
-            for (int z = 0; z < kKs; ++z) {
-              o[z][nt][y] *= keep;
-              o[z][nt][y + 2] *= keep;
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              float top = -INFINITY;
+#pragma unroll
+              for (int un = 0; un < U; ++un) top = fmaxf(top, fmaxf(x[un][nt][y], x[un][nt][y + 2]));
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+              const float to = fmaxf(m[nt][y], fmaf(top, factor[nt][y], -kAim));
+              const float keep = exp2f(m[nt][y] - to);
+              m[nt][y] = to;
+              l[nt][y] *= keep;
+#pragma unroll
+              for (int z = 0; z < kKs; ++z) {
+                o[z][nt][y] *= keep;
+                o[z][nt][y + 2] *= keep;
+              }
+            }
+        }
+#pragma unroll
+        for (int un = 0; un < U; ++un) {
+          const uint8_t* tile = tiles + un * Tile<D>::kBytes;
+          uint32_t pf[NT][PC][2];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const float p0 = exp2f(fmaf(x[un][nt][0], factor[nt][0], -m[nt][0]));
+            const float p1 = exp2f(fmaf(x[un][nt][1], factor[nt][1], -m[nt][1]));
+            const float p2 = exp2f(fmaf(x[un][nt][2], factor[nt][0], -m[nt][0]));
+            const float p3 = exp2f(fmaf(x[un][nt][3], factor[nt][1], -m[nt][1]));
+            l[nt][0] += p0 + p2;
+            l[nt][1] += p1 + p3;
+            const uint32_t top = pack2(p0, p1), low = pack2(p2, p3);
+            pf[nt][0][0] = transpose8(top);
+            pf[nt][0][1] = transpose8(low);
+            if (PC == 2) {
+              pf[nt][PC - 1][0] = transpose8(rest2(p0, p1, top));
+              pf[nt][PC - 1][1] = transpose8(rest2(p2, p3, low));
             }
           }
-      }
-#pragma unroll
-      for (int un = 0; un < U; ++un) {
-        const uint8_t* tile = tiles + un * Tile<D>::kBytes;
-        uint32_t pf[NT][PC][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float p0 = exp2f(fmaf(x[un][nt][0], factor[nt][0], -m[nt][0]));
-          const float p1 = exp2f(fmaf(x[un][nt][1], factor[nt][1], -m[nt][1]));
-          const float p2 = exp2f(fmaf(x[un][nt][2], factor[nt][0], -m[nt][0]));
-          const float p3 = exp2f(fmaf(x[un][nt][3], factor[nt][1], -m[nt][1]));
-          l[nt][0] += p0 + p2;
-          l[nt][1] += p1 + p3;
-          const uint32_t top = pack2(p0, p1), low = pack2(p2, p3);
-          pf[nt][0][0] = transpose8(top);
-          pf[nt][0][1] = transpose8(low);
-          if (PC == 2) {
-            pf[nt][PC - 1][0] = transpose8(rest2(p0, p1, top));
-            pf[nt][PC - 1][1] = transpose8(rest2(p2, p3, low));
-          }
-        }
-        // sums: keys lc, lc + 4, lc + 8, lc + 12 and the lr-th eighth of the dimensions
-        constexpr int kWords = D / 64;
-        uint32_t w[4][kWords], sv[4];           // words of a key; its scales, one byte or (D = 256) two
-#pragma unroll
-        for (int z = 0; z < 4; ++z) {
-          load_words(w[z], tile + (z & 1 ? at_v4 : at_v) + (z / 2) * 4 * D);
-          const uint8_t* vs = tile + at_vs + z * (D / 4);
-          sv[z] = D == 256 ? *reinterpret_cast<const uint16_t*>(vs) : *vs;
-        }
-        uint32_t poisoned[D == 256 ? 2 : 1] = {};     // bit: key whose values of this lane's group are NaN
-        if (!full) {
-          bool nan = false;
+          // sums: keys lc, lc + 4, lc + 8, lc + 12 and the lr-th eighth of the dimensions
+          constexpr int kWords = D / 64;
+          uint32_t w[4][kWords], sv[4];           // words of a key; its scales, one byte or (D = 256) two
 #pragma unroll
           for (int z = 0; z < 4; ++z) {
-            if (!(shown[un] >> (lc + 4 * z) & 1)) sv[z] = 0;
-            nan |= (sv[z] & 0x7f) == 0x7f || (sv[z] & 0x7f00) == 0x7f00;
+            load_words(w[z], tile + (z & 1 ? at_v4 : at_v) + (z / 2) * 4 * D);
+            const uint8_t* vs = tile + at_vs + z * (D / 4);
+            sv[z] = D == 256 ? *reinterpret_cast<const uint16_t*>(vs) : *vs;
           }
-          if (__any_sync(0xffffffffu, nan)) {
-            // 0 times NaN would reach the rows that do not see the key: taken out here, put in below
+          uint32_t poisoned[D == 256 ? 2 : 1] = {};     // bit: key whose values of this lane's group are NaN
+          if (!kFull) {
+            bool nan = false;
 #pragma unroll
-            for (int z = 0; z < 4; ++z)
+            for (int z = 0; z < 4; ++z) {
+              if (!(shown[un] >> (lc + 4 * z) & 1)) sv[z] = 0;
+              nan |= (sv[z] & 0x7f) == 0x7f || (sv[z] & 0x7f00) == 0x7f00;
+            }
+            if (__any_sync(0xffffffffu, nan)) {
+              // 0 times NaN would reach the rows that do not see the key: taken out here, put in below
 #pragma unroll
-              for (int g = 0; g < (D == 256 ? 2 : 1); ++g) {
-                const bool bad = (sv[z] >> (8 * g) & 0x7f) == 0x7f;
-                poisoned[g] |= (__ballot_sync(0xffffffffu, bad) >> (4 * lr) & 15u) << (4 * z);
-                if (bad) sv[z] &= ~(0xffu << (8 * g));
-              }
-          }
-        }
+              for (int z = 0; z < 4; ++z)
 #pragma unroll
-        for (int u = 0; u < kWords; ++u) {
-          const int g = D == 256 ? u / 2 : 0;
-          uint32_t v[2][2][4];                  // [dimension even, odd][keys lower, upper half][pair of rows]
-#pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const uint32_t a0 = w[2 * z][u], a1 = w[2 * z + 1][u];
-            const uint32_t even = (a0 & 0x0f0f0f0fu) | ((a1 << 4) & 0xf0f0f0f0u);
-            const uint32_t odd = ((a0 >> 4) & 0x0f0f0f0fu) | (a1 & 0xf0f0f0f0u);
-            const uint32_t two = scales_to_half2(__byte_perm(sv[2 * z], sv[2 * z + 1], g ? 0x0051 : 0x0040));
-            codes_to_half2(even, v[0][z]);
-            codes_to_half2(odd, v[1][z]);
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              v[0][z][y] = mul2(v[0][z][y], two);
-              v[1][z][y] = mul2(v[1][z][y], two);
+                for (int g = 0; g < (D == 256 ? 2 : 1); ++g) {
+                  const bool bad = (sv[z] >> (8 * g) & 0x7f) == 0x7f;
+                  poisoned[g] |= (__ballot_sync(0xffffffffu, bad) >> (4 * lr) & 15u) << (4 * z);
+                  if (bad) sv[z] &= ~(0xffu << (8 * g));
+                }
             }
           }
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const uint32_t fa[4] = {v[0][0][y], v[1][0][y], v[0][1][y], v[1][1][y]};
+          for (int u = 0; u < kWords; ++u) {
+            const int g = D == 256 ? u / 2 : 0;
+            uint32_t v[2][2][4];                  // [dimension even, odd][keys lower, upper half][pair of rows]
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
+            for (int z = 0; z < 2; ++z) {
+              const uint32_t a0 = w[2 * z][u], a1 = w[2 * z + 1][u];
+              const uint32_t even = (a0 & 0x0f0f0f0fu) | ((a1 << 4) & 0xf0f0f0f0u);
+              const uint32_t odd = ((a0 >> 4) & 0x0f0f0f0fu) | (a1 & 0xf0f0f0f0u);
+              const uint32_t two = scales_to_half2(__byte_perm(sv[2 * z], sv[2 * z + 1], g ? 0x0051 : 0x0040));
+              codes_to_half2(even, v[0][z]);
+              codes_to_half2(odd, v[1][z]);
 #pragma unroll
-              for (int z = PC - 1; z >= 0; --z) mma(o[4 * u + y][nt], fa, pf[nt][z][0], pf[nt][z][1]);
-          }
-        }
-        if (!full) {
+              for (int y = 0; y < 4; ++y) {
+                v[0][z][y] = mul2(v[0][z][y], two);
+                v[1][z][y] = mul2(v[1][z][y], two);
+              }
+            }
 #pragma unroll
-          for (int g = 0; g < (D == 256 ? 2 : 1); ++g)
-            if (poisoned[g])
+            for (int y = 0; y < 4; ++y) {
+              const uint32_t fa[4] = {v[0][0][y], v[1][0][y], v[0][1][y], v[1][1][y]};
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                  const int pos = en.len + (en.r0 + 8 * nt + 2 * lc + y) / p.G, first = unit + un * kStep;
-                  bool hit = false;
-                  for (int key = 0; key < kUnit; ++key)
-                    hit |= (poisoned[g] >> key & 1) && (!a.causal || first + key <= pos) &&
-                           (a.w <= 0 || pos - (first + key) < a.w);
-                  if (hit)
+                for (int z = PC - 1; z >= 0; --z) mma(o[4 * u + y][nt], fa, pf[nt][z][0], pf[nt][z][1]);
+            }
+          }
+          if (!kFull) {
 #pragma unroll
-                    for (int z = 0; z < kKs; ++z)
-                      if (D != 256 || z / 8 == g) o[z][nt][y] = o[z][nt][y + 2] = __uint_as_float(0x7fffffffu);
-                }
+            for (int g = 0; g < (D == 256 ? 2 : 1); ++g)
+              if (poisoned[g])
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                  for (int y = 0; y < 2; ++y) {
+                    const int pos = en.len + (en.r0 + 8 * nt + 2 * lc + y) / p.G, first = unit + un * kStep;
+                    bool hit = false;
+                    for (int key = 0; key < kUnit; ++key)
+                      hit |= (poisoned[g] >> key & 1) && (!a.causal || first + key <= pos) &&
+                             (a.w <= 0 || pos - (first + key) < a.w);
+                    if (hit)
+#pragma unroll
+                      for (int z = 0; z < kKs; ++z)
+                        if (D != 256 || z / 8 == g) o[z][nt][y] = o[z][nt][y + 2] = __uint_as_float(0x7fffffffu);
+                  }
+          }
         }
-      }
+      };
+      if (full) take(std::true_type());
+      else take(std::false_type());
     }
+
     // the next segment's copies start before this one is joined
     const Entry done = en;
     const int done_h = h, done_k0 = k0;
