@@ -25,22 +25,12 @@ __global__ void __launch_bounds__(32 * kWarps) attend_kernel(const Params p) {
   int e;
   int64_t before;
   const Line line = find(p, &e, &before);
-  if (e < 0) {
-    if (!p.by_segment) file_split(p, 0, 0, 0);
-    return;
-  }
-  int64_t s = line.begin(blockIdx.x);
-  const int64_t end = line.begin(blockIdx.x + 1);
+  Walk w;
   bool begins = false;
-  Entry en = entry(p, e);
-  while (s < end) {
-    while (en.n == 0 || s >= before + (int64_t)en.n * c.Hkv) {
-      before += (int64_t)en.n * c.Hkv;
-      en = entry(p, ++e);
-    }
-    const int h = (int)((s - before) / en.n);
-    const int64_t seg = before + (int64_t)h * en.n;
-    const int k0 = (int)(s - seg), k1 = (int)min((int64_t)en.n, end - seg);
+  if (!start(p, line, e, before, &w)) return file_nothing(p);
+  while (next(p, &w)) {
+    const Entry& en = w.en;
+    const int h = w.h, k0 = w.k0, k1 = w.k1;
     __syncthreads();
     for (int i = tid; i < kRows * d; i += 32 * kWarps) {
       const int r = i / d, x = i - r * d;
@@ -150,10 +140,7 @@ __global__ void __launch_bounds__(32 * kWarps) attend_kernel(const Params p) {
     __syncthreads();
     const bool whole = k0 == 0 && k1 == en.n;
     float* part = part_of(p, blockIdx.x, k0 == 0);
-    if (k0 == 0) {
-      file_split(p, e, h, whole ? 1 : line.of(seg + en.n - 1) - (int)blockIdx.x + 1);
-      begins = true;
-    }
+    begins |= file_split(p, line, w);
     for (int i = tid; i < en.rows * d; i += 32 * kWarps) {
       const int r = i / d, x = i - r * d;
       float to = -INFINITY;
@@ -178,9 +165,8 @@ __global__ void __launch_bounds__(32 * kWarps) attend_kernel(const Params p) {
         }
       }
     }
-    s = seg + k1;
   }
-  if (!begins && !p.by_segment) file_split(p, 0, 0, 0);
+  if (!begins) file_nothing(p);
 }
 
 // Joins the parts of split segments.  A CTA has eight warps for rows / gridDim.y rows of one segment; the warps

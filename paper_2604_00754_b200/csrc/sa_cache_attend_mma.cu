@@ -156,17 +156,13 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
   int e;
   int64_t before;
   const Line line = find(p, &e, &before);
-  if (e < 0) {
-    if (!p.by_segment) file_split(p, 0, 0, 0);
-    return;
-  }
-  int64_t s = line.begin(blockIdx.x);
-  const int64_t end = line.begin(blockIdx.x + 1);
+  Walk w;
+  if (!start(p, line, e, before, &w)) return file_nothing(p);
+  Entry& en = w.en;
   bool begins = false;
-  Entry en = entry(p, e);
-  // the segment at hand: head, steps [k0, k1) of it, this warp's first unit (the next is kStep on)
-  int h, k0, k1, unit0, units, turns, full_hi;
-  int64_t seg, full_lo;
+  // the portion at hand: this warp's first unit (the next is kStep on), how many, in how many turns
+  int unit0, units, turns, full_hi;
+  int64_t full_lo;
   uint2 ahead;
   const uint8_t *src_k, *src_v, *src_s;
   uint32_t there, slot;      // units of the last kTurns - 1 turns, the oldest on top; ring slot of the next turn
@@ -208,18 +204,11 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
     copies_end();
     return found;
   };
-  // finds the segment at step s and starts its first copies; the warp has read what its ring held
-  auto open = [&] {
-    while (en.n == 0 || s >= before + (int64_t)en.n * c.Hkv) {
-      before += (int64_t)en.n * c.Hkv;
-      en = entry(p, ++e);
-    }
-    h = (int)quotient(s - before, en.n);
-    seg = before + (int64_t)h * en.n;
-    k0 = (int)(s - seg);
-    k1 = (int)min((int64_t)en.n, end - seg);
-    unit0 = (en.first + k0) * kStep + warp * kUnit;
-    units = k1 - k0;
+  // takes the next portion and starts its first copies; the warp has read what its ring held
+  auto open = [&]() -> bool {
+    if (!next(p, &w)) return false;
+    unit0 = (en.first + w.k0) * kStep + warp * kUnit;
+    units = w.k1 - w.k0;
     turns = (units + U - 1) / U;
     // keys below full_hi and from full_lo on are seen by every row
     full_hi = a.causal ? min(en.len + en.t0 + 1, en.hi) : en.hi;   // (lengths and T are below 2^30)
@@ -228,10 +217,10 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
       if (8 * nt + lr < en.rows)
-        asm volatile("prefetch.global.L1 [%0];" ::"l"(row_of(p, reinterpret_cast<const T*>(a.q), a.qs, en, h, 8 * nt + lr) +
+        asm volatile("prefetch.global.L1 [%0];" ::"l"(row_of(p, reinterpret_cast<const T*>(a.q), a.qs, en, w.h, 8 * nt + lr) +
                                                      lc * (D / 4)));
     // this lane's 16-byte pieces of a unit: D / 64 of K's codes and of V's, 512 bytes apart, and one of scales
-    const uint8_t* head = c.pool + (int64_t)2 * h * c.side;
+    const uint8_t* head = c.pool + (int64_t)2 * w.h * c.side;
     src_k = head + lane * 16;
     src_v = src_k + c.side;
     src_s = head + c.P * (D / 2) + (lane < D / 16 ? 0 : c.side - D) + lane * 16;
@@ -243,10 +232,11 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
     there = slot = 0;
 #pragma unroll
     for (int i = 0; i < kTurns - 1; ++i) there = there << U | issue(i, i * U * Tile<D>::kBytes);
+    return true;
   };
 
-  open();
-  for (;;) {
+  bool more = open();
+  while (more) {
     // Q of this lane's fragments: row 8 nt + lr, the lc-th quarter of its dimensions
     uint32_t qf[S::kQInRegs ? NT : 1][PC][S::kQInRegs ? kKs : 1][2];
     float factor[NT][2];      // log2 units per unit of a score, of the two columns 2 lc, 2 lc + 1
@@ -255,7 +245,7 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
     for (int nt = 0; nt < NT; ++nt) {
       const int r = 8 * nt + lr;
       float x[D / 4];
-      const T* q = row_of(p, reinterpret_cast<const T*>(a.q), a.qs, en, h, r < en.rows ? r : 0) + lc * (D / 4);
+      const T* q = row_of(p, reinterpret_cast<const T*>(a.q), a.qs, en, w.h, r < en.rows ? r : 0) + lc * (D / 4);
       if (sizeof(T) == 2) {
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) {
@@ -426,7 +416,7 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
           }
         }
         // exponents relative to the reference m; lanes look at each other only where one has too much
-        bool more = false;
+        bool high = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -434,9 +424,9 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
             float top = -INFINITY;
 #pragma unroll
             for (int un = 0; un < U; ++un) top = fmaxf(top, fmaxf(x[un][nt][y], x[un][nt][y + 2]));
-            more |= fmaf(top, factor[nt][y], -m[nt][y]) > kMost;
+            high |= fmaf(top, factor[nt][y], -m[nt][y]) > kMost;
           }
-        if (__any_sync(0xffffffffu, more)) {
+        if (__any_sync(0xffffffffu, high)) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -561,15 +551,11 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
 
     // the next segment's copies start before this one is joined
     const Entry done = en;
-    const int done_h = h, done_k0 = k0;
-    const bool whole = k0 == 0 && k1 == en.n;
-    if (k0 == 0) {
-      file_split(p, e, h, whole ? 1 : line.of(seg + en.n - 1) - (int)blockIdx.x + 1);
-      begins = true;
-    }
-    s = seg + k1;
+    const int done_h = w.h;
+    const bool whole = w.k0 == 0 && w.k1 == en.n, first = w.k0 == 0;
+    begins |= file_split(p, line, w);
     __syncwarp();
-    if (s < end) open();
+    more = open();
 
     // the warps join: maximum and sums first, then the rows, one warp after the other
     __syncthreads();           // o_s of the last segment has been read
@@ -622,7 +608,7 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
       }
       __syncthreads();
     }
-    float* part = part_of(p, blockIdx.x, done_k0 == 0);
+    float* part = part_of(p, blockIdx.x, first);
     for (int i = tid; i < done.rows * D; i += 32 * kWarps) {
       const int r = i / D, x = i % D;
       float to = kNone, sum = 0.f;
@@ -646,9 +632,8 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT>::kCtas) attend_mm
         }
       }
     }
-    if (s >= end) break;
   }
-  if (!begins && !p.by_segment) file_split(p, 0, 0, 0);
+  if (!begins) file_nothing(p);
 }
 
 template <typename T, int D, int NT>

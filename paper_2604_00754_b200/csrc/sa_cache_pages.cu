@@ -136,24 +136,42 @@ __device__ __forceinline__ Span span_of(const Books& c, const Reserve& r, int b)
   return s;
 }
 
+// A thread's run of pages, looked at 32 at a time: bit i of a look is test(refs[q + i]), and the looks of runs up to
+// 32 pages are remembered.
+struct Run {
+  int p0, p1;
+  __device__ Run(int pages) {
+    const int run = (pages + kBook - 1) / kBook;
+    p0 = min((int)threadIdx.x * run, pages);
+    p1 = min(p0 + run, pages);
+  }
+  template <typename F>
+  __device__ uint32_t look(const int32_t* refs, int q, F&& test) const {
+    uint32_t bits = 0;
+    for (int i = 0; i < 32 && q + i < p1; i += 8)
+#pragma unroll
+      for (int k = i; k < i + 8; ++k)
+        if (q + k < p1 && test(__ldcg(refs + q + k))) bits |= 1u << k;
+    return bits;
+  }
+  __device__ bool one_look() const { return p1 - p0 <= 32; }
+};
+
 // One CTA: counts what every slot wants, gives the lowest free pages out in order, marks the moves.
 __global__ void __launch_bounds__(kBook, 1) reserve_kernel(const Books c, const Reserve r) {
   __shared__ int copies;
   grid_dependency_wait();
   const int tid = threadIdx.x;
   if (tid == 0) copies = 0;
-  // free pages: each thread has a run of them
-  const int run = (c.pages + kBook - 1) / kBook;
-  const int p0 = min(tid * run, c.pages), p1 = min(p0 + run, c.pages);
-  int mine = 0, n_free, n_want;
-  for (int p = p0; p < p1; ++p) mine += c.refs[p] == 0;
-  int at = before_me(mine, &n_free);
-  for (int p = p0; p < p1; ++p)
-    if (c.refs[p] == 0) r.free_list[at++] = p;
+  auto is_free = [](int refs) { return refs == 0; };
+  const Run run(c.pages);
+  const uint32_t first = run.look(c.refs, run.p0, is_free);
+  int free = __popc(first), n_free, n_want;
+  for (int q = run.p0 + 32; q < run.p1; q += 32) free += __popc(run.look(c.refs, q, is_free));
   // wants, in order of the slots; once one does not fit, none behind it does
   const int run_b = (c.slots + kBook - 1) / kBook;
   const int b0 = min(tid * run_b, c.slots), b1 = min(b0 + run_b, c.slots);
-  mine = 0;
+  int wants = 0;
   for (int b = b0; b < b1; ++b) {
     const Span s = span_of(c, r, b);
     const int32_t* row = c.table + (int64_t)b * c.row;
@@ -167,31 +185,37 @@ __global__ void __launch_bounds__(kBook, 1) reserve_kernel(const Books c, const 
     }
     if (bad) report(c);
     r.want[b] = s.fits && !bad ? want : -1;
-    mine += bad ? 0 : want;
+    wants += bad ? 0 : want;
   }
-  at = before_me(mine, &n_want);
-  __syncthreads();   // all have looked at the counts as they were
+  int at = before_me(free, &n_free);
+  const int at_want = before_me(wants, &n_want);      // all have looked at the counts as they were
+  if (n_want > 0)
+    for (int q = run.p0; q < run.p1; q += 32)
+      for (uint32_t bits = run.one_look() ? first : run.look(c.refs, q, is_free); bits; bits &= bits - 1)
+        r.free_list[at++] = q + __ffs(bits) - 1;
+  at = at_want;
   for (int b = b0; b < b1; ++b) {
     const int want = r.want[b];
-    const Span s = span_of(c, r, b);
-    int32_t* row = c.table + (int64_t)b * c.row;
     const bool ok = want == 0 || (want > 0 && at + want <= n_free);
     r.got[b] = ok;
-    if (ok && want)
+    if (ok && want) {
+      const Span s = span_of(c, r, b);
+      int32_t* row = c.table + (int64_t)b * c.row;
       // entries that this slot alone holds keep their page; a shared one counted above is marked
       for (int j = s.lo; j < s.hi; ++j) {
         const int p = row[j];
         if (p >= 0 && c.refs[p] > 1) row[j] = -2 - p;
       }
+    }
     at += max(want, 0);
   }
   __syncthreads();   // marks are set from the counts as they were; now the counts change
-  at = before_me(mine, &n_want);
+  at = at_want;
   for (int b = b0; b < b1; ++b) {
     const int want = r.want[b];
-    const Span s = span_of(c, r, b);
-    int32_t* row = c.table + (int64_t)b * c.row;
-    if (want > 0 && r.got[b]) {
+    if (want > 0 && at + want <= n_free) {
+      const Span s = span_of(c, r, b);
+      int32_t* row = c.table + (int64_t)b * c.row;
       int k = at;
       for (int j = s.lo; j < s.hi; ++j) {
         const int p = row[j];
@@ -248,7 +272,7 @@ __global__ void __launch_bounds__(kMove) reserve_copy_kernel(const Books c, cons
 struct Compact {
   int32_t* head;    // live, moves
   int2* moves;      // (from, to)
-  int32_t* to;      // by page: where it moves, or -1
+  int32_t* to;      // by page, from the number of live ones on: where it moves, or -1
   int32_t* live;    // nullable: caller's
 };
 
@@ -256,28 +280,32 @@ struct Compact {
 __global__ void __launch_bounds__(kBook, 1) compact_kernel(const Books c, const Compact w) {
   grid_dependency_wait();
   const int tid = threadIdx.x;
-  const int run = (c.pages + kBook - 1) / kBook;
-  const int p0 = min(tid * run, c.pages), p1 = min(p0 + run, c.pages);
-  int mine = 0, live, n;
-  for (int p = p0; p < p1; ++p) {
-    const int refs = c.refs[p];
-    mine += refs > 0;
+  auto is_held = [&](int refs) {
     if (refs < 0) report(c);
-  }
+    return refs > 0;
+  };
+  const Run run(c.pages);
+  const uint32_t first = run.look(c.refs, run.p0, is_held);
+  int mine = __popc(first), live, n;
+  for (int q = run.p0 + 32; q < run.p1; q += 32) mine += __popc(run.look(c.refs, q, is_held));
   before_me(mine, &live);
+  // of pages q .. q + 31 of the run: those below `live`, those in the run
+  auto upto = [](int count) { return count >= 32 ? ~0u : count <= 0 ? 0u : (1u << count) - 1u; };
+  auto holes_of = [&](uint32_t held, int q) { return ~held & upto(run.p1 - q) & upto(live - q); };
+  auto movers_of = [&](uint32_t held, int q) { return held & ~upto(live - q); };
   int holes = 0, movers = 0;
-  for (int p = p0; p < p1; ++p) {
-    const bool held = c.refs[p] > 0;
-    holes += p < live && !held;
-    movers += p >= live && held;
+  for (int q = run.p0; q < run.p1; q += 32) {
+    const uint32_t held = run.one_look() ? first : run.look(c.refs, q, is_held);
+    holes += __popc(holes_of(held, q));
+    movers += __popc(movers_of(held, q));
   }
   int at_hole = before_me(holes, &n), at_mover = before_me(movers, &n);
-  for (int p = p0; p < p1; ++p) {
-    const bool held = c.refs[p] > 0;
-    if (p < live && !held) w.moves[at_hole++].y = p;
-    if (p >= live && held) w.moves[at_mover++].x = p;
-    w.to[p] = -1;
+  for (int q = run.p0; q < run.p1; q += 32) {
+    const uint32_t held = run.one_look() ? first : run.look(c.refs, q, is_held);
+    for (uint32_t bits = holes_of(held, q); bits; bits &= bits - 1) w.moves[at_hole++].y = q + __ffs(bits) - 1;
+    for (uint32_t bits = movers_of(held, q); bits; bits &= bits - 1) w.moves[at_mover++].x = q + __ffs(bits) - 1;
   }
+  for (int p = live + tid; p < c.pages; p += kBook) w.to[p] = -1;
   __syncthreads();
   for (int k = tid; k < n; k += kBook) {
     const int2 m = w.moves[k];
