@@ -21,8 +21,8 @@ sa_status check_geometry(const sa_cache* c) {
     return SA_ERR_INVALID_ARG;
   if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return SA_ERR_INVALID_ARG;
   if (c->d % 16 != 0 || c->d > 256 || c->Hkv > 32767) return SA_ERR_UNSUPPORTED;
-  // positions are 32-bit
-  if ((int64_t)c->row * c->page > (1ll << 30)) return SA_ERR_UNSUPPORTED;
+  // positions and table entries are counted in 32 bits
+  if ((int64_t)c->row * c->page > (1ll << 30) || (int64_t)c->slots * c->row > 0x7fffffff) return SA_ERR_UNSUPPORTED;
   return SA_OK;
 }
 

@@ -136,26 +136,91 @@ __device__ __forceinline__ Span span_of(const Books& c, const Reserve& r, int b)
   return s;
 }
 
-// A thread's run of pages, looked at 32 at a time: bit i of a look is test(refs[q + i]), and the looks of runs up to
-// 32 pages are remembered.
+// Every lane of a warp has a slot and a span of its entries (maybe empty).  Short spans are gone through by their
+// lane, long ones (a prompt's) by the whole warp, one after the other.
+constexpr int kShort = 4;
+
+// f(entry, j) returns 1 to count the entry, -1 for a bad one; totals go to the span's own lane.
+template <typename F>
+__device__ __forceinline__ void entries_of(const Books& c, int b, const Span& s, F&& f, int* count, bool* bad) {
+  const int lane = threadIdx.x & 31;
+  int32_t* row = c.table + (int64_t)b * c.row;
+  const bool is_long = s.hi - s.lo > kShort;
+  if (!is_long)
+    for (int j = s.lo; j < s.hi; ++j) {
+      const int v = f(row + j, j);
+      *count += v > 0;
+      *bad |= v < 0;
+    }
+  for (uint32_t todo = __ballot_sync(0xffffffffu, is_long); todo; todo &= todo - 1) {
+    const int of = __ffs(todo) - 1;
+    const int lo = __shfl_sync(0xffffffffu, s.lo, of), hi = __shfl_sync(0xffffffffu, s.hi, of);
+    int32_t* r = c.table + (int64_t)__shfl_sync(0xffffffffu, b, of) * c.row;
+    for (int j0 = lo; j0 < hi; j0 += 32) {
+      const int j = j0 + lane, v = j < hi ? f(r + j, j) : 0;
+      const int n = __popc(__ballot_sync(0xffffffffu, v > 0));
+      const bool any_bad = __any_sync(0xffffffffu, v < 0);
+      if (lane == of) {
+        *count += n;
+        *bad |= any_bad;
+      }
+    }
+  }
+}
+
+// take(entry, j, k, len) for the entries whose value passes, k = first, first + 1, ... in their order.
+template <typename P, typename F>
+__device__ __forceinline__ void ranked_entries_of(const Books& c, int b, const Span& s, int first, P&& passes, F&& take) {
+  const int lane = threadIdx.x & 31;
+  int32_t* row = c.table + (int64_t)b * c.row;
+  const bool is_long = s.hi - s.lo > kShort;
+  if (!is_long) {
+    int k = first;
+    for (int j = s.lo; j < s.hi; ++j)
+      if (passes(row[j])) take(row + j, j, k++, s.len);
+  }
+  for (uint32_t todo = __ballot_sync(0xffffffffu, is_long); todo; todo &= todo - 1) {
+    const int of = __ffs(todo) - 1;
+    const int lo = __shfl_sync(0xffffffffu, s.lo, of), hi = __shfl_sync(0xffffffffu, s.hi, of);
+    const int len = __shfl_sync(0xffffffffu, s.len, of);
+    int k = __shfl_sync(0xffffffffu, first, of);
+    int32_t* r = c.table + (int64_t)__shfl_sync(0xffffffffu, b, of) * c.row;
+    for (int j0 = lo; j0 < hi; j0 += 32) {
+      const int j = j0 + lane;
+      const bool mine = j < hi && passes(r[j]);
+      const uint32_t all = __ballot_sync(0xffffffffu, mine);
+      if (mine) take(r + j, j, k + __popc(all & ((1u << lane) - 1u)), len);
+      k += __popc(all);
+    }
+  }
+}
+
+// A warp's run of pages, 32 at a time and eight of those loads on the way: f(first page of the 32, this lane's count
+// of holders, -1 behind the pool's end), called by all lanes.
 struct Run {
-  int p0, p1;
-  __device__ Run(int pages) {
-    const int run = (pages + kBook - 1) / kBook;
-    p0 = min((int)threadIdx.x * run, pages);
-    p1 = min(p0 + run, pages);
+  int p0, p1, pages;
+  __device__ Run(int n) : pages(n) {
+    const int chunks = (n + 31) / 32, per = (chunks + kBook / 32 - 1) / (kBook / 32), warp = threadIdx.x >> 5;
+    p0 = min(warp * per, chunks) * 32;
+    p1 = min((warp + 1) * per, chunks) * 32;
   }
   template <typename F>
-  __device__ uint32_t look(const int32_t* refs, int q, F&& test) const {
-    uint32_t bits = 0;
-    for (int i = 0; i < 32 && q + i < p1; i += 8)
+  __device__ __forceinline__ void each(const int32_t* refs, F&& f) const {
+    const int lane = threadIdx.x & 31;
+    for (int q = p0; q < p1; q += 256) {
+      int v[8];
 #pragma unroll
-      for (int k = i; k < i + 8; ++k)
-        if (q + k < p1 && test(__ldcg(refs + q + k))) bits |= 1u << k;
-    return bits;
+      for (int k = 0; k < 8; ++k) v[k] = q + 32 * k < p1 && q + 32 * k + lane < pages ? __ldcg(refs + q + 32 * k + lane) : -1;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (q + 32 * k < p1) f(q + 32 * k, v[k]);
+    }
   }
-  __device__ bool one_look() const { return p1 - p0 <= 32; }
 };
+// Sum of the warps' n (alike in their lanes) before this warp, and over all.
+__device__ __forceinline__ int before_warp(int n, int* total) {
+  return __shfl_sync(0xffffffffu, before_me(threadIdx.x & 31 ? 0 : n, total), 0);
+}
 
 // One CTA: counts what every slot wants, gives the lowest free pages out in order, marks the moves.
 __global__ void __launch_bounds__(kBook, 1) reserve_kernel(const Books c, const Reserve r) {
@@ -163,73 +228,70 @@ __global__ void __launch_bounds__(kBook, 1) reserve_kernel(const Books c, const 
   grid_dependency_wait();
   const int tid = threadIdx.x;
   if (tid == 0) copies = 0;
-  auto is_free = [](int refs) { return refs == 0; };
+  const uint32_t below = (1u << (tid & 31)) - 1u;      // lanes before this one
   const Run run(c.pages);
-  const uint32_t first = run.look(c.refs, run.p0, is_free);
-  int free = __popc(first), n_free, n_want;
-  for (int q = run.p0 + 32; q < run.p1; q += 32) free += __popc(run.look(c.refs, q, is_free));
+  int free = 0, n_free, n_want;
+  run.each(c.refs, [&](int, int refs) { free += __popc(__ballot_sync(0xffffffffu, refs == 0)); });
   // wants, in order of the slots; once one does not fit, none behind it does
   const int run_b = (c.slots + kBook - 1) / kBook;
   const int b0 = min(tid * run_b, c.slots), b1 = min(b0 + run_b, c.slots);
   int wants = 0;
-  for (int b = b0; b < b1; ++b) {
-    const Span s = span_of(c, r, b);
-    const int32_t* row = c.table + (int64_t)b * c.row;
+  for (int i = 0; i < run_b; ++i) {
+    const int b = b0 + i;
+    const Span s = b < b1 ? span_of(c, r, b) : Span{0, 0, 0, true};
     int want = 0;
     bool bad = false;
-    for (int j = s.lo; j < s.hi; ++j) {
-      const int p = row[j];
-      if (p == -1) ++want;
-      else if ((unsigned)p >= (unsigned)c.pages) bad = true;
-      else want += c.refs[p] > 1;
+    entries_of(c, b, s, [&](int32_t* e, int) {
+      const int p = *e;
+      if (p == -1) return 1;
+      if ((unsigned)p >= (unsigned)c.pages) return -1;
+      return c.refs[p] > 1 ? 1 : 0;
+    }, &want, &bad);
+    if (b < b1) {
+      if (bad) report(c);
+      r.want[b] = s.fits && !bad ? want : -1;
+      wants += bad ? 0 : want;
     }
-    if (bad) report(c);
-    r.want[b] = s.fits && !bad ? want : -1;
-    wants += bad ? 0 : want;
   }
-  int at = before_me(free, &n_free);
+  int at = before_warp(free, &n_free);
   const int at_want = before_me(wants, &n_want);      // all have looked at the counts as they were
-  if (n_want > 0)
-    for (int q = run.p0; q < run.p1; q += 32)
-      for (uint32_t bits = run.one_look() ? first : run.look(c.refs, q, is_free); bits; bits &= bits - 1)
-        r.free_list[at++] = q + __ffs(bits) - 1;
+  if (at < n_want)
+    run.each(c.refs, [&](int q, int refs) {
+      const uint32_t bits = __ballot_sync(0xffffffffu, refs == 0);
+      if (refs == 0) r.free_list[at + __popc(bits & below)] = q + (tid & 31);
+      at += __popc(bits);
+    });
   at = at_want;
-  for (int b = b0; b < b1; ++b) {
-    const int want = r.want[b];
+  for (int i = 0; i < run_b; ++i) {
+    const int b = b0 + i, want = b < b1 ? r.want[b] : 0;
     const bool ok = want == 0 || (want > 0 && at + want <= n_free);
-    r.got[b] = ok;
-    if (ok && want) {
-      const Span s = span_of(c, r, b);
-      int32_t* row = c.table + (int64_t)b * c.row;
-      // entries that this slot alone holds keep their page; a shared one counted above is marked
-      for (int j = s.lo; j < s.hi; ++j) {
-        const int p = row[j];
-        if (p >= 0 && c.refs[p] > 1) row[j] = -2 - p;
-      }
-    }
+    if (b < b1) r.got[b] = ok;
+    // entries that this slot alone holds keep their page; a shared one counted above is marked
+    int none = 0;
+    bool no = false;
+    entries_of(c, b, ok && want ? span_of(c, r, b) : Span{0, 0, 0, true}, [&](int32_t* e, int) {
+      const int p = *e;
+      if (p >= 0 && c.refs[p] > 1) *e = -2 - p;
+      return 0;
+    }, &none, &no);
     at += max(want, 0);
   }
   __syncthreads();   // marks are set from the counts as they were; now the counts change
   at = at_want;
-  for (int b = b0; b < b1; ++b) {
-    const int want = r.want[b];
-    if (want > 0 && at + want <= n_free) {
-      const Span s = span_of(c, r, b);
-      int32_t* row = c.table + (int64_t)b * c.row;
-      int k = at;
-      for (int j = s.lo; j < s.hi; ++j) {
-        const int p = row[j];
-        if (p >= 0) continue;
-        const int page = r.free_list[k++];
-        row[j] = page;
-        c.refs[page] = 1;
-        if (p != -1) {
-          atomicSub(&c.refs[-2 - p], 1);
-          // only the page of the last token so far has anything in it: one copy a slot at most
-          if ((int64_t)j * c.P < s.len) r.copy[atomicAdd(&copies, 1)] = make_int2(-2 - p, page);
-        }
+  for (int i = 0; i < run_b; ++i) {
+    const int b = b0 + i, want = b < b1 ? r.want[b] : 0;
+    const Span s = want > 0 && at + want <= n_free ? span_of(c, r, b) : Span{0, 0, 0, true};
+    // the k-th entry that is missing or marked takes the k-th page of this slot's
+    ranked_entries_of(c, b, s, at, [&](int p) { return p < 0; }, [&](int32_t* e, int j, int k, int len) {
+      const int p = *e, page = r.free_list[k];
+      *e = page;
+      c.refs[page] = 1;
+      if (p != -1) {
+        atomicSub(&c.refs[-2 - p], 1);
+        // only the page of the last token so far has anything in it: one copy a slot at most
+        if ((int64_t)j * c.P < len) r.copy[atomicAdd(&copies, 1)] = make_int2(-2 - p, page);
       }
-    }
+    });
     at += max(want, 0);
   }
   __syncthreads();
@@ -280,31 +342,29 @@ struct Compact {
 __global__ void __launch_bounds__(kBook, 1) compact_kernel(const Books c, const Compact w) {
   grid_dependency_wait();
   const int tid = threadIdx.x;
-  auto is_held = [&](int refs) {
-    if (refs < 0) report(c);
-    return refs > 0;
-  };
+  const uint32_t below = (1u << (tid & 31)) - 1u;      // lanes before this one
   const Run run(c.pages);
-  const uint32_t first = run.look(c.refs, run.p0, is_held);
-  int mine = __popc(first), live, n;
-  for (int q = run.p0 + 32; q < run.p1; q += 32) mine += __popc(run.look(c.refs, q, is_held));
-  before_me(mine, &live);
-  // of pages q .. q + 31 of the run: those below `live`, those in the run
-  auto upto = [](int count) { return count >= 32 ? ~0u : count <= 0 ? 0u : (1u << count) - 1u; };
-  auto holes_of = [&](uint32_t held, int q) { return ~held & upto(run.p1 - q) & upto(live - q); };
-  auto movers_of = [&](uint32_t held, int q) { return held & ~upto(live - q); };
+  int mine = 0, live, n;
+  run.each(c.refs, [&](int q, int refs) {
+    if (refs < 0 && q + (tid & 31) < c.pages) report(c);
+    mine += __popc(__ballot_sync(0xffffffffu, refs > 0));
+  });
+  before_warp(mine, &live);
+  auto is_hole = [&](int q, int refs) { return q + (tid & 31) < live && refs <= 0; };
+  auto is_mover = [&](int q, int refs) { return q + (tid & 31) >= live && refs > 0; };
   int holes = 0, movers = 0;
-  for (int q = run.p0; q < run.p1; q += 32) {
-    const uint32_t held = run.one_look() ? first : run.look(c.refs, q, is_held);
-    holes += __popc(holes_of(held, q));
-    movers += __popc(movers_of(held, q));
-  }
-  int at_hole = before_me(holes, &n), at_mover = before_me(movers, &n);
-  for (int q = run.p0; q < run.p1; q += 32) {
-    const uint32_t held = run.one_look() ? first : run.look(c.refs, q, is_held);
-    for (uint32_t bits = holes_of(held, q); bits; bits &= bits - 1) w.moves[at_hole++].y = q + __ffs(bits) - 1;
-    for (uint32_t bits = movers_of(held, q); bits; bits &= bits - 1) w.moves[at_mover++].x = q + __ffs(bits) - 1;
-  }
+  run.each(c.refs, [&](int q, int refs) {
+    holes += __popc(__ballot_sync(0xffffffffu, is_hole(q, refs)));
+    movers += __popc(__ballot_sync(0xffffffffu, is_mover(q, refs)));
+  });
+  int at_hole = before_warp(holes, &n), at_mover = before_warp(movers, &n);
+  run.each(c.refs, [&](int q, int refs) {
+    const uint32_t h = __ballot_sync(0xffffffffu, is_hole(q, refs)), m = __ballot_sync(0xffffffffu, is_mover(q, refs));
+    if (is_hole(q, refs)) w.moves[at_hole + __popc(h & below)].y = q + (tid & 31);
+    if (is_mover(q, refs)) w.moves[at_mover + __popc(m & below)].x = q + (tid & 31);
+    at_hole += __popc(h);
+    at_mover += __popc(m);
+  });
   for (int p = live + tid; p < c.pages; p += kBook) w.to[p] = -1;
   __syncthreads();
   for (int k = tid; k < n; k += kBook) {

@@ -30,7 +30,7 @@ def append(c, layer=0, B=1, T=1, k=FAKE, v=FAKE, dt=sa.BF16, st=ST, slots=None, 
 
 
 GEOMETRY = [(dict(layers=0), 1), (dict(pages=0), 1), (dict(Hkv=0), 1), (dict(page=24), 1), (dict(page=256), 1),
-            (dict(slots=0), 1), (dict(row=0), 1), (dict(d=40), 2), (dict(d=272), 2), (dict(row=1 << 26), 2),
+            (dict(slots=0), 1), (dict(row=0), 1), (dict(d=40), 2), (dict(d=272), 2), (dict(row=1 << 26), 2), (dict(slots=1 << 20, row=1 << 12), 2),
             (dict(table=None), 1), (dict(table=FAKE + 2), 1)]
 
 

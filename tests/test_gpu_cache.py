@@ -376,7 +376,8 @@ def test_bad_fork_free_reserve_are_recorded():
 
 @pytest.mark.parametrize("seed", range(6))
 @pytest.mark.parametrize("layers,Hkv,d,P,S,row,pages", [(3, 2, 32, 16, 12, 6, 60), (1, 1, 16, 64, 40, 9, 300),
-                                                        (2, 3, 128, 128, 5, 40, 130), (1, 1, 16, 16, 1500, 4, 5000)])
+                                                        (2, 3, 128, 128, 5, 40, 130), (1, 1, 16, 16, 1500, 4, 5000),
+                                                        (1, 2, 16, 16, 70, 90, 4000)])
 def test_books_follow_the_lists(seed, layers, Hkv, d, P, S, row, pages):
     rng = np.random.default_rng(seed)
     pool = torch.randint(0, 256, (layers, pages, Hkv, 2, P * (d // 2 + d // 16)), dtype=torch.uint8, device="cuda")
