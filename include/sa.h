@@ -440,7 +440,8 @@ uint64_t sa_launch_count(void);
  *   SA_DEBUG_SWA_TILE_LOADS   1 = one-sided SWA branch loads whole tiles by TMA when the layout
  *                             allows (default), 0 = always gather rows
  *   SA_DEBUG_TENSOR_CORES     1 = tensor-core kernels where they apply (default), 0 = the
- *                             general CUDA-core kernels everywhere
+ *                             general CUDA-core kernels everywhere (but in sa_cache_attend, which
+ *                             has the one kernel)
  *   SA_DEBUG_GATE_WIDE_TILES  1 = 128 x 256 tiles for large gate projections (default), 0 = the
  *                             fused 128 x 128 kernel
  * Returns SA_ERR_INVALID_ARG for an unknown key or value.  Takes effect for later calls. */

@@ -15,7 +15,7 @@ NATIVE_SRC = os.path.join(CSRC, "sa_native.cpp")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "--use_fast_math", "-Xcompiler", "-fPIC", "-shared",
+    "--use_fast_math", "-Xcompiler", "-fPIC", "-shared", "--threads", "4",
 ]
 
 

@@ -252,11 +252,8 @@ inline Params params(const AttendArgs& a, int shares, int rows) {
 
 }  // namespace attend
 
-// The second launch: joins what the shares left.
-cudaError_t launch_cache_join(const attend::Params& p, int dtype, cudaStream_t st);
-// The tensor-core kernels: whether they take the head dimension, their shape for a call, the call.
-bool cache_attend_mma_takes(int d);
-void cache_attend_mma_shape(int T, int G, int d, int dtype, int* shares, int* rows);
-cudaError_t launch_cache_attend_mma(const attend::Params& p, int dtype, cudaStream_t st);
+// Shares and rows of a tile for a call; the launch that attends, and the second, which joins what the shares left.
+void cache_attend_shape(int T, int G, int d, int dtype, int* shares, int* rows);
+cudaError_t launch_cache_attend_tiles(const attend::Params& p, int dtype, cudaStream_t st);
 
 }  // namespace sa
