@@ -16,11 +16,12 @@ cudaError_t launch_rows(const Params& p, int nt, cudaStream_t st) {
   });
 }
 
-// Row tiles of 8, 16 or 32: the smallest that holds all rows of a KV head, else 32 (16 for 256 dimensions, whose
-// sums would not fit the registers, and for padded ones): K and V are then dequantised once per tile of rows.
+// Row tiles that a warp takes of a KV head's rows: K and V are dequantised once per so many, so as many as there are or
+// fit, spread evenly (37 rows: two times three tiles, not four and one).
 int row_tiles(int T, int G, int d) {
-  const int64_t rows = (int64_t)T * G;
-  return rows <= 8 ? 1 : rows <= 16 || tile_dim(d) == 256 || tile_dim(d) != d ? 2 : 4;
+  const int most = most_tiles(tile_dim(d), tile_dim(d) != d);
+  const int64_t all = ((int64_t)T * G + 7) / 8, times = (all + most - 1) / most;
+  return (int)((all + times - 1) / times);
 }
 
 }  // namespace

@@ -694,13 +694,19 @@ cudaError_t launch(const Params& p, cudaStream_t st) {
 // Tile of a head dimension.
 inline int tile_dim(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-// f(D, NT, pad) of a head dimension and a number of row tiles, as types.
+// Row tiles of eight that a warp takes at most: of 256 dimensions two (the sums of more would not fit the registers),
+// of padded ones two (fewer kernels).
+constexpr int most_tiles(int D, bool pad) { return pad || D == 256 ? 2 : 4; }
+
+// f(D, NT) of a head dimension and a number of row tiles, as types.
 template <bool kPad, typename F>
 auto with_shape(int d, int nt, F&& f) {
   auto rows = [&](auto dim) {
-    constexpr int D = decltype(dim)::value, kMost = kPad || D == 256 ? 2 : 4;
-    return nt == 1 ? f(dim, std::integral_constant<int, 1>()) : nt == 2 ? f(dim, std::integral_constant<int, 2>())
-                                                                        : f(dim, std::integral_constant<int, kMost>());
+    constexpr int kMost = most_tiles(decltype(dim)::value, kPad);
+    return nt == 1   ? f(dim, std::integral_constant<int, 1>())
+           : nt == 2 ? f(dim, std::integral_constant<int, 2>())
+           : nt == 3 ? f(dim, std::integral_constant<int, kMost < 3 ? kMost : 3>())
+                     : f(dim, std::integral_constant<int, kMost>());
   };
   const int D = tile_dim(d);
   return D == 64 ? rows(std::integral_constant<int, 64>()) : D == 128 ? rows(std::integral_constant<int, 128>())
