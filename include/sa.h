@@ -341,7 +341,8 @@ sa_status sa_gate_projection_backward(int64_t rows, int32_t dm, int32_t dtype, c
  * have to be distinct.
  * Errors of the calls: SA_ERR_INVALID_ARG, SA_ERR_UNSUPPORTED, SA_ERR_WORKSPACE, SA_ERR_CUDA.  What only
  * the device can see (slots, counts, lengths or pages out of range, a token without a page) is
- * skipped and recorded as SA_ERR_BAD_CACHE for sa_read_status; keys without a page count as hidden. */
+ * skipped and recorded as SA_ERR_BAD_CACHE for sa_read_status; keys without a page count as hidden.
+ * The first of these calls on a device looks up the word that records it: before any stream capture. */
 typedef struct {
   uint8_t* pool;        /* 16-byte aligned                                                      */
   int32_t* table;       /* [slots, row]                                                         */
@@ -391,8 +392,8 @@ sa_status sa_cache_attend(const sa_cache* c, int32_t layer, int32_t B, int32_t T
  * length 0.  Slots have to be distinct (a second mention is recorded and does nothing). */
 sa_status sa_cache_free(const sa_cache* c, int32_t n, const int32_t* slots, sa_stream_t stream);
 
-/* Forks: child i (an empty slot) gets the pages and the length of parent i; no page is copied, each has
- * one holder more.  Several children may have one parent.  Recorded and left out: a child that is
+/* Forks: child i (an empty slot) gets the length of parent i and the pages of that length (not those reserved
+ * beyond it); no page is copied, each has one holder more.  Several children may have one parent.  Recorded and left out: a child that is
  * listed twice, is a parent as well or holds pages, a parent without the pages of its length. */
 sa_status sa_cache_fork(const sa_cache* c, int32_t n, const int32_t* parents,
                         const int32_t* children, sa_stream_t stream);
@@ -402,8 +403,8 @@ sa_status sa_cache_fork(const sa_cache* c, int32_t n, const int32_t* parents,
  * own, in all layers, before anything is written to them.  Free pages go out lowest first, to slots in
  * their order; a slot gets all that it needs or nothing, and once one did not fit none behind it gets any.
  * A page that all its holders replace in one call is free afterwards, for later calls.
- * got: out, device int32 [slots]: 1 where the room is there, 0 where it is not (no pages left, or a row
- * too short).  lens is not changed.  ws: scratch of sa_cache_ws_bytes(c), 16-byte aligned. */
+ * got: out, device int32 [slots], not add: 1 where the room is there, 0 where it is not (no pages left, or
+ * a row too short).  lens is not changed.  ws: scratch of sa_cache_ws_bytes(c), 16-byte aligned. */
 size_t sa_cache_ws_bytes(const sa_cache* c);
 sa_status sa_cache_reserve(const sa_cache* c, const int32_t* add, int32_t* got, void* ws,
                            size_t ws_bytes, sa_stream_t stream);

@@ -197,7 +197,8 @@ sa_status sa_cache_reserve(const sa_cache* c, const int32_t* add, int32_t* got, 
                            size_t ws_bytes, sa_stream_t stream) {
   const sa_status s = check_books(c, true, true, true);
   if (s != SA_OK) return s;
-  if (!ints(add) || !ints(got) || !ws || !aligned(ws, 16)) return SA_ERR_INVALID_ARG;
+  // add is read after the first of got is written
+  if (!ints(add) || !ints(got) || add == got || !ws || !aligned(ws, 16)) return SA_ERR_INVALID_ARG;
   if (ws_bytes < cache_books_ws_bytes(*c)) return SA_ERR_WORKSPACE;
   int* status = cache_status_ptr();
   if (!status) return SA_ERR_CUDA;

@@ -9,7 +9,7 @@ import torch
 import cache_ref as ref
 from paper_2604_00754_b200 import binding as sa
 
-FAKE, ODD = 0x1000, 0x1004          # never dereferenced: every case fails before a launch
+FAKE, ODD, OTHER = 0x1000, 0x1004, 0x2000          # never dereferenced: every case fails before a launch
 ST = (ctypes.c_int64 * 3)(1024, 128, 64)
 
 
@@ -71,7 +71,7 @@ def test_books_refusals():
         bad = cache(**kw)
         assert lib.sa_cache_free(r(bad), 1, FAKE, None) == expect
         assert lib.sa_cache_fork(r(bad), 1, FAKE, FAKE, None) == expect
-        assert lib.sa_cache_reserve(r(bad), FAKE, FAKE, FAKE, 1 << 30, None) == expect
+        assert lib.sa_cache_reserve(r(bad), FAKE, OTHER, FAKE, 1 << 30, None) == expect
         if "lens" not in kw:
             assert lib.sa_cache_compact(r(bad), FAKE, FAKE, 1 << 30, None) == expect
     assert lib.sa_cache_free(None, 1, FAKE, None) == 1
@@ -82,9 +82,10 @@ def test_books_refusals():
     assert lib.sa_cache_fork(r(c), 0, None, None, None) == 0
     assert lib.sa_cache_reserve(r(c), None, FAKE, FAKE, 1 << 30, None) == 1
     assert lib.sa_cache_reserve(r(c), FAKE, None, FAKE, 1 << 30, None) == 1
-    assert lib.sa_cache_reserve(r(c), FAKE, FAKE, None, 1 << 30, None) == 1
-    assert lib.sa_cache_reserve(r(c), FAKE, FAKE, FAKE, 16, None) == 3
-    assert lib.sa_cache_reserve(r(cache(pool=ODD)), FAKE, FAKE, FAKE, 1 << 30, None) == 1
+    assert lib.sa_cache_reserve(r(c), FAKE, OTHER, None, 1 << 30, None) == 1
+    assert lib.sa_cache_reserve(r(c), FAKE, FAKE, FAKE, 1 << 30, None) == 1      # add and got are one
+    assert lib.sa_cache_reserve(r(c), FAKE, OTHER, FAKE, 16, None) == 3
+    assert lib.sa_cache_reserve(r(cache(pool=ODD)), FAKE, OTHER, FAKE, 1 << 30, None) == 1
     assert lib.sa_cache_compact(r(c), FAKE, FAKE, 16, None) == 3
     assert lib.sa_cache_compact(r(c), 0x1002, FAKE, 1 << 30, None) == 1
 

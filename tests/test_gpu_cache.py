@@ -169,14 +169,15 @@ def test_attend_same_bits_again_and_from_other_memory(d):
     assert sa.sa_read_status() == 0
 
 
-@pytest.mark.parametrize("d", [64, 80, 128])
-def test_attend_values_that_are_not_finite(d):
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 80, 128, 256])
+def test_attend_values_that_are_not_finite(d, dt):
     """A NaN or an infinity reaches the rows that see it and no others."""
     rng = np.random.default_rng(2)
     pool, table, _ = filled(rng, 2, 2, d, 16, [8, 8])
     zero = ints([0, 0])
     k, v = (torch.randn(2, 2, 128, d, device="cuda") for _ in range(2))
-    q = torch.randn(2, 4, 40, d, device="cuda")
+    q = torch.randn(2, 4, 40, d, device="cuda").to(DT[dt])
     sa.sa_cache_append(pool, table, zero, k, v)
     lens = ints([60, 60])
     clean = sa.sa_cache_attend(pool, table, lens, q)
@@ -213,6 +214,47 @@ def test_attend_sizes_of_queries(dt, size):
         # the scale itself may round once more: 2^-23 of the scores
         assert (one[1] - two[1]).abs().max() < 2.0 ** -20 * (1 + one[1].abs().max())
         assert (one[0].float() - two[0].float()).abs().max() <= 2.0 ** (-7 if dt == "bf16" else -18) * v.abs().max()
+
+
+def test_attend_on_two_streams_at_once():
+    """Calls that overlap, each with a workspace of its own, do not touch each other."""
+    rng = np.random.default_rng(8)
+    jobs, streams = [], [torch.cuda.Stream() for _ in range(2)]
+    for d, dt in ((128, "bf16"), (64, "f32")):
+        pool, table, _ = filled(rng, 7, 2, d, 64, [30, 1, 2, 17, 40, 5, 8])
+        lens = ints([1900, 3, 100, 1024, 2500, 300, 512])
+        k, v = (torch.randn(7, 2, 2500, d, device="cuda").to(DT[dt]) for _ in range(2))
+        sa.sa_cache_append(pool, table, ints([0] * 7), k, v, counts=lens)
+        q = torch.randn(7, 8, 3, d, device="cuda").to(DT[dt])
+        jobs.append((pool, table, lens, q, sa.sa_cache_attend(pool, table, lens, q, flags=0)))
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(sa.sa_cache_attend(*jobs[i][:4], flags=0))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(y, jobs[i][4]) for y in got[i])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_attend_views(dt):
+    """q and y as parts of wider tensors: rows 16 bytes apart from others' values, which stay."""
+    rng = np.random.default_rng(9)
+    pool, table, _ = filled(rng, 3, 2, 64, 16, [3, 1, 5])
+    k, v = (torch.randn(3, 2, 70, 64, device="cuda").to(DT[dt]) for _ in range(2))
+    lens = ints([40, 9, 70])
+    sa.sa_cache_append(pool, table, ints([0, 0, 0]), k, v, counts=lens)
+    wide = torch.randn(3, 2, 12 * 64 + 8, device="cuda").to(DT[dt])          # a fused projection's output
+    q = wide[:, :, 8:8 + 8 * 64].view(3, 2, 8, 64).transpose(1, 2)
+    out = torch.full((3, 2, 8, 72), 7.0, dtype=DT[dt], device="cuda")
+    y = out[..., :64].transpose(1, 2)
+    sa.sa_cache_attend(pool, table, lens, q, flags=0, y=y)
+    assert torch.equal(y, sa.sa_cache_attend(pool, table, lens, q.contiguous(), flags=0)) and (out[..., 64:] == 7).all()
+    one = sa.sa_cache_attend(pool, table, lens, q[:, :, :1], flags=0)        # one token: any token stride
+    assert torch.equal(one, y[:, :, :1])
+    assert sa.sa_read_status() == 0
 
 
 # ---- append and read
