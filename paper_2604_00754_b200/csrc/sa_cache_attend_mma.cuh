@@ -562,9 +562,20 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT, kPad>::kCtas) att
             for (int y = 0; y < 4; ++y) {
               const uint32_t fa[4] = {v[0][0][y], v[1][0][y], v[0][1][y], v[1][1][y]};
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
+              for (int nt = 0; nt < NT; ++nt) {
+                float(&sum)[4] = o[4 * u + y][nt];
+                if (PC == 1) {
+                  mma(sum, fa, pf[nt][0][0], pf[nt][0][1]);
+                } else {
+                  // the tensor core cuts its sums off: over a unit that is nothing, over thousands of keys in one
+                  // accumulator it was 3e-6 of an fp32 result; the running sum is rounded
+                  float t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int z = PC - 1; z >= 0; --z) mma(o[4 * u + y][nt], fa, pf[nt][z][0], pf[nt][z][1]);
+                  for (int z = PC - 1; z >= 0; --z) mma(t, fa, pf[nt][z][0], pf[nt][z][1]);
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) sum[k] += t[k];
+                }
+              }
             }
           }
           if (!kFull) {

@@ -216,6 +216,25 @@ def test_attend_sizes_of_queries(dt, size):
         assert (one[0].float() - two[0].float()).abs().max() <= 2.0 ** (-7 if dt == "bf16" else -18) * v.abs().max()
 
 
+@pytest.mark.parametrize("d", [64, 128, 80])
+def test_attend_fp32_sums_over_many_keys(d):
+    """fp32 over 6000 keys, by so many sequences (of the same pages) that one CTA goes through all keys of a head.
+
+    Errors of keys are independent: 2^-22 |score| of the score (|score| < 8) and 2^-22 of the exponential, below 2^-19
+    of each term p v, and the running sum is rounded, not cut off: relative to the sum, whose terms have both signs as
+    the errors have, 2^-19 too."""
+    n, B, Hkv = 6000, 120, 4
+    pool, table, _ = filled(np.random.default_rng(3), 1, Hkv, d, 128, [-(-n // 128)])
+    k, v = torch.randn(1, Hkv, n, d, device="cuda") * 0.5, torch.randn(1, Hkv, n, d, device="cuda")
+    sa.sa_cache_append(pool, table, ints([0]), k, v)
+    sa.sa_cache_read(pool, table, k, v)
+    q = torch.randn(B, 2 * Hkv, 1, d, device="cuda")
+    y = sa.sa_cache_attend(pool, table.expand(B, -1).contiguous(), ints([n] * B), q, flags=0).double()
+    s = (q.double().view(B, Hkv, 2, d) @ k.double().transpose(2, 3)) / d ** 0.5
+    want = (s.softmax(-1) @ v.double()).view(B, 2 * Hkv, 1, d)
+    assert (y - want).norm() <= 2.0 ** -19 * want.norm()
+
+
 def test_attend_on_two_streams_at_once():
     """Calls that overlap, each with a workspace of its own, do not touch each other."""
     rng = np.random.default_rng(8)
