@@ -8,7 +8,7 @@ namespace {
 
 // Joins the parts of split segments.  A CTA has eight warps for rows / gridDim.y rows of one segment; the warps
 // of a row take every so-many-th part, each with a maximum of its own, and join in their order.  A part
-// is an L2 access away: four of them are on the way at once.
+// is an L2 access away: four of them are on the way at once (111 parts of 32 rows of 128: 8.8 us, one at a time 19.4).
 constexpr int kJoinWarps = 8, kAtOnce = 4;
 
 template <typename T, int J>

@@ -6,6 +6,10 @@
 // between HBM and the multiply has to keep up with 23 bytes = 41 values per clock and SM.  A warp takes 16
 // keys of each step alone, from its copies to its own running maximum, sum and rows: no barrier stands
 // in the loop, the four warps of a CTA join once per segment.
+// 32 sequences of 32768 keys, 32/8 heads of 128 (1.21 GB): 229 us, 82 % of the copy bandwidth (260 when the power cap holds
+// the clock at 1755 MHz).  What holds it back is the work itself: per warp and 16 keys of 128 dimensions 64
+// conversions, 64 products with scales, 16 matrix instructions and 160 others, the ALU half busy, three warps per
+// scheduler.
 //   - Copies: cp.async into a ring of the warp's own (pages are contiguous per head and side: 16-byte pieces).
 //   - Scores as S^T = K Q^T: the keys are the 16 rows of mma.m16n8k16, eight query rows its columns, so that
 //     a group of 8 heads or fewer wastes no row of K.  A lane's codes become fp16 by the hardware
@@ -32,7 +36,8 @@ namespace sa {
 namespace attend {
 
 constexpr float kAim = 12.f, kMost = 15.75f;   // log2 of the largest P where the reference is set, and may be
-constexpr float kNone = -1e30f;                // reference before the first key
+constexpr float kNone = -3.4028235e38f;        // reference before the first key: any score is more
+constexpr float kLarge = 16777216.f;           // 2^24: the rounding of a reference is 1/2 at most below it
 
 template <int D>
 struct Tile {                    // a warp's 16 keys
@@ -113,10 +118,10 @@ struct Shape {
   static constexpr int kUnits = D < 256 && NT == 1 ? 2 : 1;
   static constexpr int kTurns = kUnits == 2 ? (D == 64 ? 3 : 2) : D == 64 ? 6 : D == 128 ? 4 : 3;
   static constexpr int kRing = kTurns * kUnits * Tile<D>::kBytes;
-  // CTAs per SM: what registers (rows of O, Q, the tile in flight) and shared memory leave.  64 registers of O:
+  // CTAs per SM: what registers (rows of O, Q, the tile in flight) and shared memory leave.  With 64 registers of O
   // two CTAs without spills beat three with them in one tile of rows and in four (16 x 8192 keys, 16/4 heads of 256
-  // 45.9 against 46.8 us, 37 fp32 rows over 2500 keys of 16 heads of 64 64.8 against 70.7), not in two (four
-  // tokens over 16 x 8192 keys, 32/8 heads of 128: 67.1 against 64.2).
+  // 45.9 against 46.8 us; four tiles of fp32 rows over 9 x 2500 keys of 16 heads of 64 64.8 against 70.7), not in
+  // two (four tokens over 16 x 8192 keys, 32/8 heads of 128: 67.1 against 64.2).
   static constexpr int kORegs = kKs * 4 * NT;
   static constexpr int kCtas = kORegs + (kQInRegs ? kKs * 2 * NT * PC : 0) <= 40 ? 4
                                : kORegs < 64 || (kORegs == 64 && NT == 2) ? 3 : 2;
@@ -265,6 +270,7 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT, kPad>::kCtas) att
 
   bool more = open();
   while (more) {
+    bool plain = true;        // no score of these rows can pass kLarge
     // Q of this lane's fragments: row 8 nt + lr, the lc-th quarter of its dimensions
     uint32_t qf[S::kQInRegs ? NT : 1][PC][S::kQInRegs ? kKs : 1][2];
     float factor[NT][2];      // log2 units per unit of a score, of the two columns 2 lc, 2 lc + 1
@@ -298,10 +304,17 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT, kPad>::kCtas) att
         }
       }
       uint32_t top = 0;
+      float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < D / 4; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+      for (int i = 0; i < D / 4; ++i) {
+        top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+        sum += fabsf(x[i]);
+      }
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      plain &= sum * p.scale2 <= kLarge / 2688.f;      // 2688: the largest code times the largest scale
       // the row's largest becomes 2^14 .. 2^15; rows with an infinity or NaN, and zero ones, stay
       const int ex = (int)(top >> 23) - 127;
       const int up = ex == 128 || ex == -127 ? 0 : min(14 - ex, 126);
@@ -332,6 +345,7 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT, kPad>::kCtas) att
     }
     if (!S::kQInRegs) __syncthreads();
 
+    plain = __all_sync(0xffffffffu, plain);
     float m[NT][2], l[NT][2], o[kKs][NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -361,7 +375,7 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT, kPad>::kCtas) att
       const uint32_t here = there >> (U * (kTurns - 1)) & ((1u << U) - 1u);
       if (here == 0) continue;
       const int unit = unit0 + turn * (U * kStep);
-      const bool full = here == (1u << U) - 1u && unit >= full_lo && unit + (U - 1) * kStep + kUnit <= full_hi;
+      const bool full = plain && here == (1u << U) - 1u && unit >= full_lo && unit + (U - 1) * kStep + kUnit <= full_hi;
       // two copies of the code: where every row sees every key, no branch stands between what can overlap
       auto take = [&](auto seen_by_all) {
         constexpr bool kFull = decltype(seen_by_all)::value;
@@ -452,29 +466,40 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT, kPad>::kCtas) att
               }
           }
         }
-        // exponents relative to the reference m; lanes look at each other only where one has too much
+        // Exponents relative to the reference m; lanes look at each other only where one has too much.  A score's
+        // product and the difference are one rounding, which needs a reference whose own rounding is small; the
+        // copy for masked tiles, which also takes rows that may have larger ones, rounds their products as the
+        // reference was.
+        auto exponent = [&](float score, int nt, int y) {
+          if (!kFull && fabsf(m[nt][y]) > kLarge) return __fmul_rn(score, factor[nt][y]) - m[nt][y];
+          return fmaf(score, factor[nt][y], -m[nt][y]);
+        };
+        auto top_of = [&](int nt, int y) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int un = 0; un < U; ++un) top = fmaxf(top, fmaxf(x[un][nt][y], x[un][nt][y + 2]));
+          return top;
+        };
         bool high = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            float top = -INFINITY;
-#pragma unroll
-            for (int un = 0; un < U; ++un) top = fmaxf(top, fmaxf(x[un][nt][y], x[un][nt][y + 2]));
-            high |= fmaf(top, factor[nt][y], -m[nt][y]) > kMost;
-          }
+          for (int y = 0; y < 2; ++y) high |= exponent(top_of(nt, y), nt, y) > kMost;
         if (__any_sync(0xffffffffu, high)) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              float top = -INFINITY;
-#pragma unroll
-              for (int un = 0; un < U; ++un) top = fmaxf(top, fmaxf(x[un][nt][y], x[un][nt][y + 2]));
+              float top = top_of(nt, y);
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
               top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-              const float to = fmaxf(m[nt][y], fmaf(top, factor[nt][y], -kAim));
+              float to = fmaf(top, factor[nt][y], -kAim);
+              if (!kFull) {
+                const float score = __fmul_rn(top, factor[nt][y]);
+                if (fabsf(score) > kLarge) to = score - (score - kAim) > kMost ? score : score - kAim;   // 12 may be less than a unit
+              }
+              to = fmaxf(m[nt][y], to);
               const float keep = exp2f(m[nt][y] - to);
               m[nt][y] = to;
               l[nt][y] *= keep;
@@ -491,10 +516,8 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT, kPad>::kCtas) att
           uint32_t pf[NT][PC][2];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            const float p0 = exp2f(fmaf(x[un][nt][0], factor[nt][0], -m[nt][0]));
-            const float p1 = exp2f(fmaf(x[un][nt][1], factor[nt][1], -m[nt][1]));
-            const float p2 = exp2f(fmaf(x[un][nt][2], factor[nt][0], -m[nt][0]));
-            const float p3 = exp2f(fmaf(x[un][nt][3], factor[nt][1], -m[nt][1]));
+            const float p0 = exp2f(exponent(x[un][nt][0], nt, 0)), p1 = exp2f(exponent(x[un][nt][1], nt, 1));
+            const float p2 = exp2f(exponent(x[un][nt][2], nt, 0)), p3 = exp2f(exponent(x[un][nt][3], nt, 1));
             l[nt][0] += p0 + p2;
             l[nt][1] += p1 + p3;
             const uint32_t top = pack2(p0, p1), low = pack2(p2, p3);

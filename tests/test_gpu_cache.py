@@ -276,6 +276,24 @@ def test_attend_views(dt):
     assert sa.sa_read_status() == 0
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 80, 128, 256])
+def test_attend_scores_of_any_size(d, dt):
+    """Scores up to 1e36, all of one sign: the largest takes everything, whatever its sign."""
+    rng = np.random.default_rng(10)
+    pool, table, _ = filled(rng, 1, 1, d, 16, [19])
+    k, v = torch.randn(1, 1, 300, d, device="cuda").abs(), torch.randn(1, 1, 300, d, device="cuda")
+    q = (torch.randn(1, 4, 2, d, device="cuda").abs() * 1e34).to(DT[dt])
+    for sign in (1, -1):
+        sa.sa_cache_append(pool, table, ints([0]), sign * k, v)
+        ks, vs = torch.empty_like(k), torch.empty_like(v)
+        sa.sa_cache_read(pool, table, ks, vs)
+        s = f64(q)[0] @ f64(ks)[0, 0].T * d ** -0.5
+        y, lse = sa.sa_cache_attend(pool, table, ints([300]), q, flags=0, want_lse=True)
+        assert np.array_equal(f64(y)[0], f64(vs.to(DT[dt]))[0, 0][s.argmax(-1)])
+        assert (np.abs(f64(lse)[0] - s.max(-1)) <= 2.0 ** -20 * np.abs(s).max(-1)).all()
+
+
 # ---- append and read
 
 def hard_values(rng, shape, dt):
