@@ -376,7 +376,7 @@ sa_status sa_cache_read(const sa_cache* c, int32_t layer, int32_t B, int32_t T, 
  *     j <= position     with SA_CAUSAL: the new tokens' own keys have been appended,
  *     j <  lens[slot]   without: the cached prefix alone, for joining with the tokens' own attention,
  *     and position - j < w   if w > 0.
- * q: [B,Hq,T,d], q_stride; y: out, y_stride; both dtype; rows 16-byte aligned, strides multiples of 8
+ * q: [B,Hq,T,d], q_stride; y: out, y_stride, no memory of q; both dtype; rows 16-byte aligned, strides multiples of 8
  * elements.  lse: out, nullable, contiguous fp32 [B,Hq,T].  A row that sees nothing gets y = 0 and
  * lse = -infinity.  softmax_scale 0 selects 1/sqrt(d).  flags: 0 or SA_CAUSAL.
  * ws: scratch of sa_cache_attend_ws_bytes(c, B, T, Hq, dtype) bytes, 16-byte aligned, contents of no

@@ -80,7 +80,7 @@ sa_status rows(const sa_cache* c, bool read, int32_t layer, int32_t B, int32_t T
                const int32_t* counts, sa_stream_t stream) {
   const sa_status s = check_rows(c, layer, B, T, dtype, !read);
   if (s != SA_OK) return s;
-  if (!k || !v || !aligned(k, 16) || !aligned(v, 16) || !good_strides(stride, c->d, T) ||
+  if (!k || !v || (read && k == v) || !aligned(k, 16) || !aligned(v, 16) || !good_strides(stride, c->d, T) ||
       !ints_or_null(slots) || !ints_or_null(starts) || !ints_or_null(counts))
     return SA_ERR_INVALID_ARG;
   int* status = cache_status_ptr();
@@ -139,7 +139,7 @@ sa_status sa_cache_attend(const sa_cache* c, int32_t layer, int32_t B, int32_t T
       std::isinf(softmax_scale))
     return SA_ERR_INVALID_ARG;
   if (!attend_fits(c, B, T, Hq)) return SA_ERR_UNSUPPORTED;
-  if (!q || !y || !ws || !aligned(q, 16) || !aligned(y, 16) || !aligned(ws, 16) || !ints_or_null(lse) ||
+  if (!q || !y || q == y || !ws || !aligned(q, 16) || !aligned(y, 16) || !aligned(ws, 16) || !ints_or_null(lse) ||
       !ints_or_null(slots) || !ints_or_null(counts) || !good_strides(q_stride, c->d, T) ||
       !good_strides(y_stride, c->d, T))
     return SA_ERR_INVALID_ARG;

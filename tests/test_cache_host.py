@@ -20,7 +20,7 @@ def cache(**kw):
 
 
 def attend(c, layer=0, B=1, T=1, Hq=4, q=FAKE, dt=sa.BF16, qs=ST, slots=None, counts=None, w=0, flags=1, scale=0.0,
-           y=FAKE, ys=ST, lse=None, ws=FAKE, ws_bytes=1 << 40):
+           y=OTHER, ys=ST, lse=None, ws=FAKE, ws_bytes=1 << 40):
     return sa.load_library().sa_cache_attend(ctypes.byref(c), layer, B, T, Hq, q, dt, qs, slots, counts, w, flags,
                                              scale, y, ys, lse, ws, ws_bytes, None)
 
@@ -45,7 +45,7 @@ def test_bad_caches_are_refused(kw, expect):
 
 @pytest.mark.parametrize("kw,expect", [
     (dict(layer=2), 1), (dict(layer=-1), 1), (dict(B=0), 1), (dict(T=0), 1), (dict(Hq=3), 1), (dict(Hq=0), 1),
-    (dict(q=None), 1), (dict(q=ODD), 1), (dict(y=None), 1), (dict(y=ODD), 1), (dict(dt=2), 1), (dict(w=-1), 1),
+    (dict(q=None), 1), (dict(q=ODD), 1), (dict(y=None), 1), (dict(y=ODD), 1), (dict(y=FAKE), 1), (dict(dt=2), 1), (dict(w=-1), 1),
     (dict(flags=2), 1), (dict(flags=5), 1), (dict(scale=-1.0), 1), (dict(scale=float("nan")), 1),
     (dict(scale=float("inf")), 1), (dict(lse=0x1002), 1), (dict(slots=0x1001), 1), (dict(counts=0x1001), 1),
     (dict(qs=None), 1), (dict(qs=(ctypes.c_int64 * 3)(1024, 128, 60)), 1), (dict(T=2, qs=(ctypes.c_int64 * 3)(0, 0, 56)), 1),
@@ -62,6 +62,11 @@ def test_append_and_read_refusals(kw, expect):
     assert append(cache(), **kw) == expect
     a = dict(layer=0, B=1, T=1, k=FAKE, v=FAKE, dt=sa.BF16, st=ST) | kw
     assert sa.load_library().sa_cache_read(ctypes.byref(cache(lens=None)), *a.values(), None, None, None, None) == expect
+
+
+def test_one_tensor_for_both_outputs_is_refused():
+    a = dict(layer=0, B=1, T=1, k=FAKE, v=FAKE, dt=sa.BF16, st=ST)
+    assert sa.load_library().sa_cache_read(ctypes.byref(cache()), *a.values(), None, None, None, None) == 1
 
 
 def test_books_refusals():
