@@ -8,8 +8,9 @@ namespace {
 
 // Joins the parts of split segments.  A CTA has eight warps for rows / gridDim.y rows of one segment; the warps
 // of a row take every so-many-th part, each with a maximum of its own, and join in their order.  A part
-// is an L2 access away: four of them are on the way at once (111 parts of 32 rows of 128: 8.8 us, one at a time 19.4).
-constexpr int kJoinWarps = 8, kAtOnce = 4;
+// is an L2 access away: eight of them are on the way at once (one of 131072 keys,
+// 111 parts per head: 28.6 us in all, 30.2 with four; the join alone 8.8 with four, 19.4 one at a time).
+constexpr int kJoinWarps = 8, kAtOnce = 8;
 
 template <typename T, int J>
 __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const Params p) {
