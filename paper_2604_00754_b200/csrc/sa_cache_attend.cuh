@@ -199,7 +199,7 @@ __device__ __forceinline__ float row_lse(float m, float l) {
   return l > 0.f || l != l ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 __device__ __forceinline__ float row_scale(float l, float v_scale) {
-  return l > 0.f || l != l ? v_scale / l : 0.f;
+  return l > 0.f || l != l ? __fdiv_rn(v_scale, l) : 0.f;
 }
 
 template <typename T>
