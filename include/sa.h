@@ -360,7 +360,8 @@ size_t sa_cache_page_bytes(const sa_cache* c);
  * dtype SA_F32 or SA_BF16) into a layer, at positions lens[slot] + t.  Per token, head and 16
  * dimensions, with x over t: scale = e4m3(min(max|x| / 6, 448)), code = e2m1(x / scale) saturating at
  * 6, both to the nearest with ties to even, decided exactly; 16 values with an infinity or a NaN among
- * them read back as NaN.  lens is not changed. */
+ * them read back as NaN.  lens is not changed.  The pages written to have to be the slot's alone, or a branch
+ * that shares them changes with it: sa_cache_reserve sees to that. */
 sa_status sa_cache_append(const sa_cache* c, int32_t layer, int32_t B, int32_t T, const void* k,
                           const void* v, int32_t dtype, const int64_t kv_stride[3],
                           const int32_t* slots, const int32_t* counts, sa_stream_t stream);
