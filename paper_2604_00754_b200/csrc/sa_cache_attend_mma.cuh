@@ -25,7 +25,8 @@
 // 2^-31 of the row's largest; fp32 goes as two fp16 terms (22 bits and a remainder below 2^-24).  P is taken
 // relative to a reference that keeps it between 2^12 and 2^15.75 at its largest (small ones stay normal in
 // fp16, and the reference seldom moves); it is rounded once to 11 bits in bf16 calls, below the rounding of
-// y, and goes as two terms in fp32 calls.  All sums are fp32.
+// y, and goes as two terms in fp32 calls.  All sums are fp32; the matrix instruction cuts its own off, so fp32 calls
+// add 16 dimensions of a score and 16 keys of a row in the instruction and the rest by rounded additions.
 #pragma once
 
 #include <type_traits>
@@ -431,17 +432,26 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT, kPad>::kCtas) att
               const uint32_t fa[4] = {v[0][2 * y], v[1][2 * y], v[0][2 * y + 1], v[1][2 * y + 1]};
               const int ks = 2 * u + y;
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
+              for (int nt = 0; nt < NT; ++nt) {
+                // the tensor core cuts its sums off: 32 of them in one accumulator (256 dimensions, two terms) took up to
+                // 1.1e-6 of an fp32 score, always towards 0; so each 16 dimensions have their own, and are added rounded
+                float t[4] = {0.f, 0.f, 0.f, 0.f};
+                float(&sum)[4] = PC == 1 ? x[un][nt] : t;
 #pragma unroll
                 for (int z = PC - 1; z >= 0; --z) {
                   if (S::kQInRegs) {
                     const auto& f = qf[nt % (S::kQInRegs ? NT : 1)][z][ks % (S::kQInRegs ? kKs : 1)];
-                    mma(x[un][nt], fa, f[0], f[1]);
+                    mma(sum, fa, f[0], f[1]);
                   } else {
                     const uint2 f = q_s[((nt * PC + z) * kKs + ks) * 32 + lane];
-                    mma(x[un][nt], fa, f.x, f.y);
+                    mma(sum, fa, f.x, f.y);
                   }
                 }
+                if (PC == 2) {
+#pragma unroll
+                  for (int k = 0; k < 4; ++k) x[un][nt][k] += t[k];
+                }
+              }
             }
           }
         }
@@ -590,8 +600,8 @@ __global__ void __launch_bounds__(32 * kWarps, Shape<T, D, NT, kPad>::kCtas) att
                 if (PC == 1) {
                   mma(sum, fa, pf[nt][0][0], pf[nt][0][1]);
                 } else {
-                  // the tensor core cuts its sums off: over a unit that is nothing, over thousands of keys in one
-                  // accumulator it was 3e-6 of an fp32 result; the running sum is rounded
+                  // as the scores: over a unit the cut is nothing, over thousands of keys in one accumulator it was
+                  // 3e-6 of an fp32 result; the running sum is rounded
                   float t[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                   for (int z = PC - 1; z >= 0; --z) mma(t, fa, pf[nt][z][0], pf[nt][z][1]);
