@@ -333,21 +333,22 @@ sa_status sa_gate_projection_backward(int64_t rows, int32_t dm, int32_t dtype, c
  * An empty cache: table all -1, lens and refs 0; pool may hold anything.
  *
  * A step of a model:  sa_cache_reserve makes room for the new tokens; per layer sa_cache_append writes
- * their K and V behind lens and sa_cache_attend reads all; then the caller adds the tokens to lens.
+ * their K and V behind lens and sa_cache_attend reads all; then the caller adds the tokens to lens.  Slots
+ * that reserve had no room for (got 0) take no part in it: counts times got, on the device.
  *
  * Lists: `slots` (nullable, device int32 [B]) gives the table row of each sequence of a call, without
  * it sequence b is row b.  `counts` (nullable, device int32 [B]) gives the new tokens of each sequence,
  * the first counts[b] of T; what stands behind them is neither read nor written.  Slots of an append
  * have to be distinct.
  * Errors of the calls: SA_ERR_INVALID_ARG, SA_ERR_UNSUPPORTED, SA_ERR_WORKSPACE, SA_ERR_CUDA.  What only
- * the device can see (slots, counts, lengths or pages out of range, a token without a page) is
+ * the device can see (slots, counts, lengths or pages out of range, a token without a page of its own) is
  * skipped and recorded as SA_ERR_BAD_CACHE for sa_read_status; keys without a page count as hidden.
  * The first of these calls on a device looks up the word that records it: before any stream capture. */
 typedef struct {
   uint8_t* pool;        /* 16-byte aligned                                                      */
   int32_t* table;       /* [slots, row]                                                         */
   int32_t* lens;        /* [slots]                                                              */
-  int32_t* refs;        /* [pages]; only read by reserve, fork, free, compact                   */
+  int32_t* refs;        /* [pages]; for reserve, fork, free, compact, and (nullable) append     */
   int32_t layers, pages, Hkv, d;   /* d: a multiple of 16, at most 256                          */
   int32_t page, slots, row;        /* page: 16, 32, 64 or 128 tokens                            */
   float k_scale, v_scale;          /* powers of two, 2^-32 .. 2^32                              */
@@ -360,8 +361,9 @@ size_t sa_cache_page_bytes(const sa_cache* c);
  * dtype SA_F32 or SA_BF16) into a layer, at positions lens[slot] + t.  Per token, head and 16
  * dimensions, with x over t: scale = e4m3(min(max|x| / 6, 448)), code = e2m1(x / scale) saturating at
  * 6, both to the nearest with ties to even, decided exactly; 16 values with an infinity or a NaN among
- * them read back as NaN.  lens is not changed.  The pages written to have to be the slot's alone, or a branch
- * that shares them changes with it: sa_cache_reserve sees to that. */
+ * them read back as NaN.  lens is not changed.  The pages written to have to be the slot's alone:
+ * sa_cache_reserve sees to that, where it says 1.  With c->refs a token whose page has other holders is
+ * recorded as SA_ERR_BAD_CACHE and skipped; without (null) their sequences change with it. */
 sa_status sa_cache_append(const sa_cache* c, int32_t layer, int32_t B, int32_t T, const void* k,
                           const void* v, int32_t dtype, const int64_t kv_stride[3],
                           const int32_t* slots, const int32_t* counts, sa_stream_t stream);

@@ -572,10 +572,11 @@ def sa_cache_pool(layers: int, pages: int, Hkv: int, page: int, d: int, device="
 
 
 def sa_cache_append(pool, table, lens, k, v, layer=0, slots=None, counts=None, k_scale=2.0 ** -4,
-                    v_scale=2.0 ** -4):
+                    v_scale=2.0 ** -4, refs=None):
     """Quantises k, v ([B,Hkv,T,d]) into a layer, token t of sequence b at position lens[slot] + t.
-    slots, counts: int32 [B] or None (row b; all T).  Pages must be there (sa_cache_reserve); lens stays."""
-    return (_nat or load_native()).cache_append(pool, table, lens, k, v, layer, slots, counts, k_scale, v_scale)
+    slots, counts: int32 [B] or None (row b; all T).  Pages must be there, the slot's alone (sa_cache_reserve);
+    lens stays.  With refs tokens whose page others hold too are left out and recorded, without they overwrite it."""
+    return (_nat or load_native()).cache_append(pool, table, lens, k, v, layer, slots, counts, k_scale, v_scale, refs)
 
 
 def sa_cache_read(pool, table, k, v, layer=0, slots=None, starts=None, counts=None, k_scale=2.0 ** -4,

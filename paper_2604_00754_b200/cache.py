@@ -5,15 +5,17 @@ the four tensors of that cache and calls the C entry points ``sa_cache_*`` on th
 
 A step of a model with some running sequences::
 
-    got = cache.reserve(add)                    # add: int32 [slots], the new tokens of each slot
+    new = add * cache.reserve(add)              # add: int32 [slots], the new tokens of each slot; none without room
+    counts = new[slots]                         # slots: int32 [B], the sequences of the step
     for layer in range(layers):
         ...                                     # q, k, v: [B, H, T, d] of the new tokens
         cache.append(layer, k, v, slots, counts)
         y = cache.attend(layer, q, slots, counts)
-    cache.advance(add)
+    cache.advance(new)
 
-Every call only enqueues work, so such a step can be captured into a CUDA graph; lengths and pages are read when it
-runs.  Rotary embedding comes before ``append`` and ``attend``: the tokens of a step in token-major layout are a
+Every call only enqueues work, so such a step can be captured into a CUDA graph; lengths, pages and who has room are
+read when it runs.  A sequence without room stays as it was (its rows of y: undefined): try again after others
+have left.  Rotary embedding comes before ``append`` and ``attend``: the tokens of a step in token-major layout are a
 [1, H, B*T, d] view for ``sa_rope_apply``, with the table's rows gathered at the tokens' positions.
 """
 from __future__ import annotations
@@ -49,11 +51,13 @@ class KVCache:
 
     def reserve(self, add: torch.Tensor) -> torch.Tensor:
         """Room for add[s] tokens (int32 [slots]) behind each slot's; int32 [slots]: 1 where it is there.  Slots
-        without room must not be appended to."""
+        without room (the pool or the slot's row is full) take no part in the step: counts and ``advance`` times the result."""
         return sa.sa_cache_reserve(self.pool, self.table, self.lens, self.refs, add, self.page)
 
     def append(self, layer: int, k, v, slots=None, counts=None):
-        sa.sa_cache_append(self.pool, self.table, self.lens, k, v, layer, slots, counts, self.k_scale, self.v_scale)
+        """Tokens without a page of their slot's own are left out and recorded (``sa_read_status``)."""
+        sa.sa_cache_append(self.pool, self.table, self.lens, k, v, layer, slots, counts, self.k_scale, self.v_scale,
+                           self.refs)
 
     def attend(self, layer: int, q, slots=None, counts=None, w=0, flags=sa.CAUSAL, scale=0.0, y=None, want_lse=False,
                lse=None):

@@ -115,7 +115,8 @@ struct AttendArgs {
 
 cudaError_t launch_cache_rows(const CacheView& c, bool read, int B, int T, void* k, void* v,
                               int dtype, const int64_t stride[3], const int32_t* slots,
-                              const int32_t* starts, const int32_t* counts, cudaStream_t st);
+                              const int32_t* starts, const int32_t* counts, const int32_t* refs,
+                              cudaStream_t st);
 cudaError_t launch_cache_attend(const AttendArgs& a, int dtype, cudaStream_t st);
 size_t cache_attend_ws_bytes(int B, int T, int Hq, int Hkv, int d, int dtype);
 

@@ -81,12 +81,12 @@ sa_status rows(const sa_cache* c, bool read, int32_t layer, int32_t B, int32_t T
   const sa_status s = check_rows(c, layer, B, T, dtype, !read);
   if (s != SA_OK) return s;
   if (!k || !v || (read && k == v) || !aligned(k, 16) || !aligned(v, 16) || !good_strides(stride, c->d, T) ||
-      !ints_or_null(slots) || !ints_or_null(starts) || !ints_or_null(counts))
+      !ints_or_null(slots) || !ints_or_null(starts) || !ints_or_null(counts) || (!read && !ints_or_null(c->refs)))
     return SA_ERR_INVALID_ARG;
   int* status = cache_status_ptr();
   if (!status) return SA_ERR_CUDA;
   return launch_cache_rows(view(c, layer, status), read, B, T, k, v, dtype, stride, slots, starts, counts,
-                           (cudaStream_t)stream) == cudaSuccess ? SA_OK : SA_ERR_CUDA;
+                           read ? nullptr : c->refs, (cudaStream_t)stream) == cudaSuccess ? SA_OK : SA_ERR_CUDA;
 }
 
 bool good_heads(const sa_cache* c, int32_t Hq) { return Hq >= c->Hkv && Hq % c->Hkv == 0 && Hq <= 65535; }

@@ -28,6 +28,7 @@ struct RowArgs {
   void *k, *v;
   int64_t s0, s1, s2;
   const int32_t *slots, *starts, *counts;
+  const int32_t* refs;         // of an append, nullable: holders of the pages
   int T, groups, per, loops;   // 16-dimension groups of a row, tokens of a CTA at a time, how many times
   float over[2];               // 1 / t of K and V
 };
@@ -56,7 +57,8 @@ __device__ __forceinline__ bool work_of(const RowArgs& a, Work* w) {
   return w->first >= 0;
 }
 
-// Codes and scale byte of a token's group in the pool; false: it has no page (recorded).
+// Codes and scale byte of a token's group in the pool; false (recorded): it has no page, or an append would write
+// into one that other sequences hold too.
 struct Place {
   uint8_t *codes, *scale;
 };
@@ -65,6 +67,10 @@ __device__ __forceinline__ bool place_of(const RowArgs& a, const Work& w, int t,
   const int64_t pos = (int64_t)w.first + t;
   const int page = cache_page(c, w.slot, pos);
   if (page < 0) return false;
+  if (a.refs && a.refs[page] > 1) {
+    report_cache(c);
+    return false;
+  }
   uint8_t* base = const_cast<uint8_t*>(cache_side(c, page, w.h, w.side));
   const int i = (int)pos & (c.P - 1);
   r->codes = base + i * (c.d / 2) + w.g * 8;
@@ -243,8 +249,9 @@ cudaError_t launch(const RowArgs& a, bool read, dim3 grid, cudaStream_t st) {
 
 cudaError_t launch_cache_rows(const CacheView& c, bool read, int B, int T, void* k, void* v,
                               int dtype, const int64_t stride[3], const int32_t* slots,
-                              const int32_t* starts, const int32_t* counts, cudaStream_t st) {
-  RowArgs a{c, k, v, stride[0], stride[1], stride[2], slots, starts, counts, T};
+                              const int32_t* starts, const int32_t* counts, const int32_t* refs,
+                              cudaStream_t st) {
+  RowArgs a{c, k, v, stride[0], stride[1], stride[2], slots, starts, counts, refs, T};
   a.groups = c.d / 16;
   a.per = kThreads / a.groups < T ? kThreads / a.groups : T;
   a.over[0] = 1.f / c.k_scale;

@@ -402,11 +402,14 @@ Rows rows(const at::Tensor& pool, const at::Tensor& table, const at::Tensor* len
   return r;
 }
 
-// cache_append(pool, table, lens, k, v, layer, slots, counts, k_scale, v_scale)
+// cache_append(pool, table, lens, k, v, layer, slots, counts, k_scale, v_scale, refs)
 PyObject* cache_append(PyObject* const* a) {
   const at::Tensor &pool = tensor(a[0]), &k = tensor(a[3]), &v = tensor(a[4]);
   const at::Tensor *slots = tensor_or_null(a[6]), *counts = tensor_or_null(a[7]);
-  const Rows r = rows(pool, tensor(a[1]), &tensor(a[2]), k, v, {slots, counts}, a[8], a[9], false);
+  Rows r = rows(pool, tensor(a[1]), &tensor(a[2]), k, v, {slots, counts}, a[8], a[9], false);
+  const at::Tensor* refs = tensor_or_null(a[10]);
+  ints(refs, {r.c.pages}, pool, "refs must be contiguous int32 [pages] on the cache's device");
+  r.c.refs = int_ptr(refs);
   const c10::cuda::CUDAGuard guard(pool.device());
   check(unlocked(sa_cache_append, &r.c, (int32_t)integer(a[5]), r.B, r.T, ptr(k), ptr(v), rows_dtype(k), r.st.s,
                  int_ptr(slots), int_ptr(counts), stream()),
@@ -570,7 +573,7 @@ PyMethodDef g_methods[] = {
     SA_FAST(forward, 11),
     SA_FAST(gated_forward, 16),
     SA_FAST(backward, 19),
-    SA_FAST(cache_append, 10),
+    SA_FAST(cache_append, 11),
     SA_FAST(cache_read, 10),
     SA_FAST(cache_attend, 16),
     SA_FAST(cache_free, 4),
