@@ -567,33 +567,50 @@ def sa_swa_gated_forward_host(q, k, v, gate_logits, y, w, flags, seed, layer, ws
 # refs: int32 [pages].  sa.h has the layout and what each call does; cache.KVCache holds the four.
 
 def sa_cache_pool(layers: int, pages: int, Hkv: int, page: int, d: int, device="cuda") -> torch.Tensor:
-    """A pool of the right shape, contents of no matter."""
-    return torch.empty(layers, pages, Hkv, 2, page * (d // 2 + d // 16), dtype=torch.uint8, device=device)
+    """A pool of the right shape, contents of no matter.  The tensor says how many tokens its pages hold (sa_page)."""
+    pool = torch.empty(layers, pages, Hkv, 2, page * (d // 2 + d // 16), dtype=torch.uint8, device=device)
+    pool.sa_page = page
+    return pool
+
+
+def _page(pool, page):
+    """Tokens per page of the calls below: `page`, or what the pool says.  A pool that says nothing (one that
+    sa_cache_pool did not make, a view or a copy) leaves it to the head dimension of the tensors, right or wrong:
+    64 tokens of 128 dimensions are as many bytes as 128 of 64."""
+    known = getattr(pool, "sa_page", None)
+    if page is None:
+        return known
+    if known is not None and known != page:
+        raise ValueError("the pool was made for %d tokens per page, not %d" % (known, page))
+    return page
 
 
 def sa_cache_append(pool, table, lens, k, v, layer=0, slots=None, counts=None, k_scale=2.0 ** -4,
-                    v_scale=2.0 ** -4, refs=None):
+                    v_scale=2.0 ** -4, refs=None, page=None):
     """Quantises k, v ([B,Hkv,T,d]) into a layer, token t of sequence b at position lens[slot] + t.
     slots, counts: int32 [B] or None (row b; all T).  Pages must be there, the slot's alone (sa_cache_reserve);
-    lens stays.  With refs tokens whose page others hold too are left out and recorded, without they overwrite it."""
-    return (_nat or load_native()).cache_append(pool, table, lens, k, v, layer, slots, counts, k_scale, v_scale, refs)
+    lens stays.  With refs tokens whose page others hold too are left out and recorded, without they overwrite it.
+    page: tokens per page, here and below; needed where the pool does not say it."""
+    return (_nat or load_native()).cache_append(pool, table, lens, k, v, layer, slots, counts, k_scale, v_scale, refs,
+                                                _page(pool, page))
 
 
 def sa_cache_read(pool, table, k, v, layer=0, slots=None, starts=None, counts=None, k_scale=2.0 ** -4,
-                  v_scale=2.0 ** -4):
+                  v_scale=2.0 ** -4, page=None):
     """Reads tokens starts[b] + t (from 0 without starts) back into k, v ([B,Hkv,T,d]); returns them."""
-    return (_nat or load_native()).cache_read(pool, table, k, v, layer, slots, starts, counts, k_scale, v_scale)
+    return (_nat or load_native()).cache_read(pool, table, k, v, layer, slots, starts, counts, k_scale, v_scale,
+                                              _page(pool, page))
 
 
 def sa_cache_attend(pool, table, lens, q, layer=0, slots=None, counts=None, w=0, flags=CAUSAL, scale=0.0,
-                    k_scale=2.0 ** -4, v_scale=2.0 ** -4, y=None, want_lse=False, lse=None, ws=None):
+                    k_scale=2.0 ** -4, v_scale=2.0 ** -4, y=None, want_lse=False, lse=None, ws=None, page=None):
     """Attention of the T newest tokens q ([B,Hq,T,d]) over a layer of the cache; returns y (and lse).
 
     Token t has position lens[slot] + t; it sees the keys up to its own (CAUSAL, the new tokens appended) or
     those before lens (flags 0), of them the last w if w > 0.  A row without keys: y = 0, lse = -inf.
     Rows t >= counts[b] of y and lse are left as they were (a fresh y: undefined)."""
     return (_nat or load_native()).cache_attend(pool, table, lens, q, layer, slots, counts, w, flags, scale,
-                                                k_scale, v_scale, y, want_lse, lse, ws)
+                                                k_scale, v_scale, y, want_lse, lse, ws, _page(pool, page))
 
 
 def sa_cache_free(table, lens, refs, slots):
@@ -609,7 +626,7 @@ def sa_cache_fork(table, lens, refs, parents, children, page: int):
 def sa_cache_reserve(pool, table, lens, refs, add, page: int, got=None, ws=None):
     """Makes room for add[s] tokens (int32 [slots]) behind lens[s]: pages taken, shared ones copied.
     Returns got, int32 [slots]: 1 where the room is there."""
-    return (_nat or load_native()).cache_reserve(pool, table, lens, refs, add, page, got, ws)
+    return (_nat or load_native()).cache_reserve(pool, table, lens, refs, add, _page(pool, page), got, ws)
 
 
 def sa_cache_compact(pool, table, refs, live=None, ws=None):

@@ -57,16 +57,17 @@ class KVCache:
     def append(self, layer: int, k, v, slots=None, counts=None):
         """Tokens without a page of their slot's own are left out and recorded (``sa_read_status``)."""
         sa.sa_cache_append(self.pool, self.table, self.lens, k, v, layer, slots, counts, self.k_scale, self.v_scale,
-                           self.refs)
+                           self.refs, self.page)
 
     def attend(self, layer: int, q, slots=None, counts=None, w=0, flags=sa.CAUSAL, scale=0.0, y=None, want_lse=False,
                lse=None):
         return sa.sa_cache_attend(self.pool, self.table, self.lens, q, layer, slots, counts, w, flags, scale,
-                                  self.k_scale, self.v_scale, y, want_lse, lse)
+                                  self.k_scale, self.v_scale, y, want_lse, lse, page=self.page)
 
     def read(self, layer: int, k, v, slots=None, starts=None, counts=None):
         """Tokens starts[b] + t (from 0) of a layer into k, v: a cached prefix for a prefill that goes on from it."""
-        return sa.sa_cache_read(self.pool, self.table, k, v, layer, slots, starts, counts, self.k_scale, self.v_scale)
+        return sa.sa_cache_read(self.pool, self.table, k, v, layer, slots, starts, counts, self.k_scale, self.v_scale,
+                                self.page)
 
     def advance(self, add: torch.Tensor):
         """The appended tokens count from now on (int32 [slots])."""

@@ -317,9 +317,11 @@ sa_cache cache(const at::Tensor* pool, const at::Tensor& table, const at::Tensor
   c.lens = int_ptr(lens);
   if (pool) {
     if (pool->scalar_type() != at::kByte || pool->dim() != 5 || pool->size(3) != 2 || !pool->is_contiguous() ||
-        pool->device() != table.device() || pool->size(4) != page * (d / 2 + d / 16))
+        pool->device() != table.device())
       raise(PyExc_ValueError,
             "pool must be contiguous uint8 [layers, pages, Hkv, 2, page * (d/2 + d/16)] on the table's device");
+    if (d % 16 || pool->size(4) != page * (d / 2 + d / 16))
+      raise(PyExc_ValueError, "the pool's pages do not hold that many tokens of this head dimension");
     c.pool = (uint8_t*)pool->data_ptr();
     c.layers = (int32_t)pool->size(0);
     c.pages = (int32_t)pool->size(1);
@@ -332,7 +334,11 @@ sa_cache cache(const at::Tensor* pool, const at::Tensor& table, const at::Tensor
   return c;
 }
 
-int64_t page_of(const at::Tensor& pool, int64_t d) { return pool.dim() == 5 && d ? pool.size(4) * 16 / (9 * d) : 0; }
+// Tokens per page: what the caller says, else what the pool's bytes make of the tensors' head dimension.
+int64_t page_of(const at::Tensor& pool, int64_t d, PyObject* page) {
+  if (page != Py_None) return integer(page);
+  return pool.dim() == 5 && d ? pool.size(4) * 16 / (9 * d) : 0;
+}
 
 int rows_dtype(const at::Tensor& t) {
   if (t.scalar_type() == at::kFloat) return SA_F32;
@@ -381,7 +387,7 @@ struct Rows {
 };
 Rows rows(const at::Tensor& pool, const at::Tensor& table, const at::Tensor* lens, const at::Tensor& k,
           const at::Tensor& v, std::initializer_list<const at::Tensor*> lists, PyObject* k_scale,
-          PyObject* v_scale, bool written) {
+          PyObject* v_scale, PyObject* page, bool written) {
   if (k.dim() != 4 || v.sizes() != k.sizes() || v.scalar_type() != k.scalar_type() ||
       k.device() != pool.device() || v.device() != pool.device())
     raise(PyExc_ValueError, "k and v must be [B,Hkv,T,d] of one type on the cache's device");
@@ -392,7 +398,7 @@ Rows rows(const at::Tensor& pool, const at::Tensor& table, const at::Tensor* len
     if (r.st.s[i] != sv.s[i]) raise(PyExc_ValueError, "k and v must share their strides");
   r.B = (int32_t)k.size(0);
   r.T = (int32_t)k.size(2);
-  r.c = cache(&pool, table, lens, nullptr, page_of(pool, k.size(3)), k.size(3));
+  r.c = cache(&pool, table, lens, nullptr, page_of(pool, k.size(3), page), k.size(3));
   r.c.k_scale = (float)real(k_scale);
   r.c.v_scale = (float)real(v_scale);
   if (k.size(1) != r.c.Hkv) raise(PyExc_ValueError, "k and v must have the pool's heads");
@@ -402,11 +408,11 @@ Rows rows(const at::Tensor& pool, const at::Tensor& table, const at::Tensor* len
   return r;
 }
 
-// cache_append(pool, table, lens, k, v, layer, slots, counts, k_scale, v_scale, refs)
+// cache_append(pool, table, lens, k, v, layer, slots, counts, k_scale, v_scale, refs, page)
 PyObject* cache_append(PyObject* const* a) {
   const at::Tensor &pool = tensor(a[0]), &k = tensor(a[3]), &v = tensor(a[4]);
   const at::Tensor *slots = tensor_or_null(a[6]), *counts = tensor_or_null(a[7]);
-  Rows r = rows(pool, tensor(a[1]), &tensor(a[2]), k, v, {slots, counts}, a[8], a[9], false);
+  Rows r = rows(pool, tensor(a[1]), &tensor(a[2]), k, v, {slots, counts}, a[8], a[9], a[11], false);
   const at::Tensor* refs = tensor_or_null(a[10]);
   ints(refs, {r.c.pages}, pool, "refs must be contiguous int32 [pages] on the cache's device");
   r.c.refs = int_ptr(refs);
@@ -417,11 +423,11 @@ PyObject* cache_append(PyObject* const* a) {
   return pass(Py_None);
 }
 
-// cache_read(pool, table, k, v, layer, slots, starts, counts, k_scale, v_scale)
+// cache_read(pool, table, k, v, layer, slots, starts, counts, k_scale, v_scale, page)
 PyObject* cache_read(PyObject* const* a) {
   const at::Tensor &pool = tensor(a[0]), &k = tensor(a[2]), &v = tensor(a[3]);
   const at::Tensor *slots = tensor_or_null(a[5]), *starts = tensor_or_null(a[6]), *counts = tensor_or_null(a[7]);
-  const Rows r = rows(pool, tensor(a[1]), nullptr, k, v, {slots, starts, counts}, a[8], a[9], true);
+  const Rows r = rows(pool, tensor(a[1]), nullptr, k, v, {slots, starts, counts}, a[8], a[9], a[10], true);
   const c10::cuda::CUDAGuard guard(pool.device());
   check(unlocked(sa_cache_read, &r.c, (int32_t)integer(a[4]), r.B, r.T, ptr(k), ptr(v), rows_dtype(k), r.st.s,
                  int_ptr(slots), int_ptr(starts), int_ptr(counts), stream()),
@@ -430,12 +436,12 @@ PyObject* cache_read(PyObject* const* a) {
 }
 
 // cache_attend(pool, table, lens, q, layer, slots, counts, w, flags, scale, k_scale, v_scale, y, want_lse,
-//              lse, ws)
+//              lse, ws, page)
 PyObject* cache_attend(PyObject* const* a) {
   const at::Tensor &pool = tensor(a[0]), &table = tensor(a[1]), &q = tensor(a[3]);
   if (q.dim() != 4 || q.device() != pool.device())
     raise(PyExc_ValueError, "q must be [B,Hq,T,d] on the cache's device");
-  sa_cache c = cache(&pool, table, &tensor(a[2]), nullptr, page_of(pool, q.size(3)), q.size(3));
+  sa_cache c = cache(&pool, table, &tensor(a[2]), nullptr, page_of(pool, q.size(3), a[16]), q.size(3));
   c.k_scale = (float)real(a[10]);
   c.v_scale = (float)real(a[11]);
   const int dtype = rows_dtype(q);
@@ -573,9 +579,9 @@ PyMethodDef g_methods[] = {
     SA_FAST(forward, 11),
     SA_FAST(gated_forward, 16),
     SA_FAST(backward, 19),
-    SA_FAST(cache_append, 11),
-    SA_FAST(cache_read, 10),
-    SA_FAST(cache_attend, 16),
+    SA_FAST(cache_append, 12),
+    SA_FAST(cache_read, 11),
+    SA_FAST(cache_attend, 17),
     SA_FAST(cache_free, 4),
     SA_FAST(cache_fork, 6),
     SA_FAST(cache_reserve, 8),
