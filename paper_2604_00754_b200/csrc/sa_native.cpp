@@ -292,6 +292,22 @@ PyObject* backward(PyObject* const* a) {
 
 // ---- 4-bit paged cache ----
 
+// A number that the C call takes in 32 bits, signed or not: refused here where it would lose some.
+long long small(PyObject* o) {
+  PyObject* i = PyLong_CheckExact(o) ? o : PyNumber_Long(o);
+  if (!i) throw Raised{};
+  int over = 0;
+  const long long v = PyLong_AsLongLongAndOverflow(i, &over);
+  if (i != o) Py_DECREF(i);
+  if (over || v < -(1ll << 31) || v >= (1ll << 32))
+    raise(PyExc_ValueError, "layer, w, flags and page must be numbers of 32 bits");
+  return v;
+}
+int32_t extent(const at::Tensor& t, int i) {
+  if (t.size(i) > 0x7fffffff) raise(PyExc_ValueError, "a dimension of 2^31 or more");
+  return (int32_t)t.size(i);
+}
+
 void ints(const at::Tensor* t, at::IntArrayRef sizes, const at::Tensor& like, const char* text) {
   if (t && (t->scalar_type() != at::kInt || t->sizes() != sizes || !t->is_contiguous() ||
             t->device() != like.device()))
@@ -336,7 +352,7 @@ sa_cache cache(const at::Tensor* pool, const at::Tensor& table, const at::Tensor
 
 // Tokens per page: what the caller says, else what the pool's bytes make of the tensors' head dimension.
 int64_t page_of(const at::Tensor& pool, int64_t d, PyObject* page) {
-  if (page != Py_None) return integer(page);
+  if (page != Py_None) return small(page);
   return pool.dim() == 5 && d ? pool.size(4) * 16 / (9 * d) : 0;
 }
 
@@ -383,11 +399,11 @@ at::Tensor scratch(PyObject* given, size_t need, const at::Tensor& like, const c
 struct Rows {
   sa_cache c;
   Strides st;
-  int32_t B, T;
+  int32_t B, T, layer;
 };
 Rows rows(const at::Tensor& pool, const at::Tensor& table, const at::Tensor* lens, const at::Tensor& k,
           const at::Tensor& v, std::initializer_list<const at::Tensor*> lists, PyObject* k_scale,
-          PyObject* v_scale, PyObject* page, bool written) {
+          PyObject* v_scale, PyObject* page, PyObject* layer, bool written) {
   if (k.dim() != 4 || v.sizes() != k.sizes() || v.scalar_type() != k.scalar_type() ||
       k.device() != pool.device() || v.device() != pool.device())
     raise(PyExc_ValueError, "k and v must be [B,Hkv,T,d] of one type on the cache's device");
@@ -396,15 +412,15 @@ Rows rows(const at::Tensor& pool, const at::Tensor& table, const at::Tensor* len
   const Strides sv = row_strides(v, written);
   for (int i = 0; i < 3; ++i)
     if (r.st.s[i] != sv.s[i]) raise(PyExc_ValueError, "k and v must share their strides");
-  r.B = (int32_t)k.size(0);
-  r.T = (int32_t)k.size(2);
+  r.B = extent(k, 0);
+  r.T = extent(k, 2);
+  r.layer = (int32_t)small(layer);
   r.c = cache(&pool, table, lens, nullptr, page_of(pool, k.size(3), page), k.size(3));
   r.c.k_scale = (float)real(k_scale);
   r.c.v_scale = (float)real(v_scale);
   if (k.size(1) != r.c.Hkv) raise(PyExc_ValueError, "k and v must have the pool's heads");
   for (const at::Tensor* t : lists)
     ints(t, {k.size(0)}, table, "slots, starts and counts must be contiguous int32 [B] on the cache's device");
-  on_gpu(pool);
   return r;
 }
 
@@ -412,12 +428,13 @@ Rows rows(const at::Tensor& pool, const at::Tensor& table, const at::Tensor* len
 PyObject* cache_append(PyObject* const* a) {
   const at::Tensor &pool = tensor(a[0]), &k = tensor(a[3]), &v = tensor(a[4]);
   const at::Tensor *slots = tensor_or_null(a[6]), *counts = tensor_or_null(a[7]);
-  Rows r = rows(pool, tensor(a[1]), &tensor(a[2]), k, v, {slots, counts}, a[8], a[9], a[11], false);
+  Rows r = rows(pool, tensor(a[1]), &tensor(a[2]), k, v, {slots, counts}, a[8], a[9], a[11], a[5], false);
   const at::Tensor* refs = tensor_or_null(a[10]);
   ints(refs, {r.c.pages}, pool, "refs must be contiguous int32 [pages] on the cache's device");
   r.c.refs = int_ptr(refs);
+  on_gpu(pool);
   const c10::cuda::CUDAGuard guard(pool.device());
-  check(unlocked(sa_cache_append, &r.c, (int32_t)integer(a[5]), r.B, r.T, ptr(k), ptr(v), rows_dtype(k), r.st.s,
+  check(unlocked(sa_cache_append, &r.c, r.layer, r.B, r.T, ptr(k), ptr(v), rows_dtype(k), r.st.s,
                  int_ptr(slots), int_ptr(counts), stream()),
         "sa_cache_append");
   return pass(Py_None);
@@ -427,9 +444,10 @@ PyObject* cache_append(PyObject* const* a) {
 PyObject* cache_read(PyObject* const* a) {
   const at::Tensor &pool = tensor(a[0]), &k = tensor(a[2]), &v = tensor(a[3]);
   const at::Tensor *slots = tensor_or_null(a[5]), *starts = tensor_or_null(a[6]), *counts = tensor_or_null(a[7]);
-  const Rows r = rows(pool, tensor(a[1]), nullptr, k, v, {slots, starts, counts}, a[8], a[9], a[10], true);
+  const Rows r = rows(pool, tensor(a[1]), nullptr, k, v, {slots, starts, counts}, a[8], a[9], a[10], a[4], true);
+  on_gpu(pool);
   const c10::cuda::CUDAGuard guard(pool.device());
-  check(unlocked(sa_cache_read, &r.c, (int32_t)integer(a[4]), r.B, r.T, ptr(k), ptr(v), rows_dtype(k), r.st.s,
+  check(unlocked(sa_cache_read, &r.c, r.layer, r.B, r.T, ptr(k), ptr(v), rows_dtype(k), r.st.s,
                  int_ptr(slots), int_ptr(starts), int_ptr(counts), stream()),
         "sa_cache_read");
   return tuple({pass(a[2]), pass(a[3])});
@@ -449,7 +467,9 @@ PyObject* cache_attend(PyObject* const* a) {
   const at::Tensor *slots = tensor_or_null(a[5]), *counts = tensor_or_null(a[6]);
   for (const at::Tensor* t : {slots, counts})
     ints(t, {q.size(0)}, table, "slots and counts must be contiguous int32 [B] on the cache's device");
-  const int32_t B = (int32_t)q.size(0), Hq = (int32_t)q.size(1), T = (int32_t)q.size(2);
+  const int32_t B = extent(q, 0), Hq = extent(q, 1), T = extent(q, 2);
+  const int32_t layer = (int32_t)small(a[4]), w = (int32_t)small(a[7]);
+  const uint32_t flags = (uint32_t)small(a[8]);
   const at::Tensor *y_in = tensor_or_null(a[12]), *lse_in = tensor_or_null(a[14]);
   if (y_in && (y_in->sizes() != q.sizes() || y_in->scalar_type() != q.scalar_type() || y_in->device() != q.device()))
     raise(PyExc_ValueError, "y must have the shape and type of q");
@@ -467,9 +487,8 @@ PyObject* cache_attend(PyObject* const* a) {
   const Strides ys = row_strides(y.t ? *y.t : y.own, true);
   Out lse;
   if (has_lse) lse = output(a[14], [&] { return rows_f32(q); });
-  check(unlocked(sa_cache_attend, &c, (int32_t)integer(a[4]), B, T, Hq, ptr(q), dtype, qs.s, int_ptr(slots),
-                 int_ptr(counts), (int32_t)integer(a[7]), (uint32_t)integer(a[8]), (float)real(a[9]), ptr(y), ys.s,
-                 has_lse ? (float*)ptr(lse) : nullptr, ws, bytes, stream()),
+  check(unlocked(sa_cache_attend, &c, layer, B, T, Hq, ptr(q), dtype, qs.s, int_ptr(slots), int_ptr(counts), w,
+                 flags, (float)real(a[9]), ptr(y), ys.s, has_lse ? (float*)ptr(lse) : nullptr, ws, bytes, stream()),
         "sa_cache_attend");
   return has_lse ? tuple({y.result(), lse.result()}) : y.result();
 }
@@ -494,7 +513,7 @@ PyObject* cache_free(PyObject* const* a) {
 // cache_fork(table, lens, refs, parents, children, page)
 PyObject* cache_fork(PyObject* const* a) {
   const at::Tensor& table = tensor(a[0]);
-  const sa_cache c = cache(nullptr, table, &tensor(a[1]), &tensor(a[2]), integer(a[5]), 16);
+  const sa_cache c = cache(nullptr, table, &tensor(a[1]), &tensor(a[2]), small(a[5]), 16);
   const at::Tensor &parents = list_of(a[3], table), &children = list_of(a[4], table);
   if (parents.numel() != children.numel())
     raise(PyExc_ValueError, "parents and children must have one length");
@@ -513,7 +532,7 @@ int64_t head_dim(const at::Tensor& pool, int64_t page) {
 // cache_reserve(pool, table, lens, refs, add, page, got, ws)
 PyObject* cache_reserve(PyObject* const* a) {
   const at::Tensor &pool = tensor(a[0]), &table = tensor(a[1]), &add = tensor(a[4]);
-  const int64_t page = integer(a[5]);
+  const int64_t page = small(a[5]);
   const sa_cache c = cache(&pool, table, &tensor(a[2]), &tensor(a[3]), page, head_dim(pool, page));
   ints(&add, {c.slots}, table, "add must be contiguous int32 [slots] on the cache's device");
   ints(tensor_or_null(a[6]), {c.slots}, table, "got must be contiguous int32 [slots] on the cache's device");

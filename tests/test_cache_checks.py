@@ -76,3 +76,32 @@ def test_the_right_head_dimension_gets_as_far_as_the_device(kw):
             sa.sa_cache_read(p, table, rows(64), rows(64), **kw)
         with pytest.raises(ValueError, match="must be on a CUDA device"):
             sa.sa_cache_attend(p, table, lens, rows(64), **kw)
+
+
+# ---- numbers that the C calls take in 32 bits
+
+@pytest.mark.parametrize("kw", [dict(layer=1 << 32), dict(layer=-(1 << 32)), dict(w=(1 << 32) + 5), dict(flags=1 << 33),
+                                dict(layer=1 << 70), dict(page=(1 << 32) + 16)])
+def test_numbers_past_32_bits_are_refused(kw):
+    pool, (table, lens) = sa.sa_cache_pool(1, 4, 2, 16, 64, device="cpu").clone(), books()
+    with pytest.raises(ValueError, match="numbers of 32 bits"):
+        sa.sa_cache_attend(pool, table, lens, rows(64), **kw)
+    if not {"w", "flags"} & set(kw):
+        with pytest.raises(ValueError, match="numbers of 32 bits"):
+            sa.sa_cache_append(pool, table, lens, rows(64), rows(64), **kw)
+        with pytest.raises(ValueError, match="numbers of 32 bits"):
+            sa.sa_cache_read(pool, table, rows(64), rows(64), **kw)
+    if "page" in kw:
+        refs = torch.zeros(4, dtype=torch.int32)
+        with pytest.raises(ValueError, match="numbers of 32 bits"):
+            sa.sa_cache_reserve(pool, table, lens, refs, lens.clone(), **kw)
+        with pytest.raises(ValueError, match="numbers of 32 bits"):
+            sa.sa_cache_fork(table, lens, refs, lens[:1], lens[1:], **kw)
+
+
+def test_batches_past_32_bits_are_refused():
+    pool, (table, lens) = sa.sa_cache_pool(1, 4, 2, 16, 64, device="cpu"), books()
+    many = rows(64)[:1].expand((1 << 32) + 1, 2, 1, 64)
+    for call in (lambda: sa.sa_cache_append(pool, table, lens, many, many), lambda: sa.sa_cache_attend(pool, table, lens, many)):
+        with pytest.raises(ValueError, match="a dimension of 2.31 or more"):
+            call()
