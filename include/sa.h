@@ -369,7 +369,7 @@ sa_status sa_cache_append(const sa_cache* c, int32_t layer, int32_t B, int32_t T
                           const int32_t* slots, const int32_t* counts, sa_stream_t stream);
 
 /* Reads tokens starts[b] + t (starts nullable: from 0), t < counts[b] or T, of a layer back into k, v:
- * out, [B,Hkv,T,d].  Exact for values within the type.  Reads pages, not lens. */
+ * out, [B,Hkv,T,d], rows apart from each other.  Exact for values within the type.  Reads pages, not lens. */
 sa_status sa_cache_read(const sa_cache* c, int32_t layer, int32_t B, int32_t T, void* k, void* v,
                         int32_t dtype, const int64_t kv_stride[3], const int32_t* slots,
                         const int32_t* starts, const int32_t* counts, sa_stream_t stream);
@@ -379,7 +379,7 @@ sa_status sa_cache_read(const sa_cache* c, int32_t layer, int32_t B, int32_t T, 
  *     j <= position     with SA_CAUSAL: the new tokens' own keys have been appended,
  *     j <  lens[slot]   without: the cached prefix alone, for joining with the tokens' own attention,
  *     and position - j < w   if w > 0.
- * q: [B,Hq,T,d], q_stride; y: out, y_stride, no memory of q; both dtype; rows 16-byte aligned, strides multiples of 8
+ * q: [B,Hq,T,d], q_stride; y: out, y_stride, no memory of q, rows apart from each other; both dtype; rows 16-byte aligned, strides multiples of 8
  * elements.  lse: out, nullable, contiguous fp32 [B,Hq,T].  A row that sees nothing gets y = 0 and
  * lse = -infinity.  softmax_scale 0 selects 1/sqrt(d).  flags: 0 or SA_CAUSAL.
  * ws: scratch of sa_cache_attend_ws_bytes(c, B, T, Hq, dtype) bytes, 16-byte aligned, contents of no

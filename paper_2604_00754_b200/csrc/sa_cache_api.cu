@@ -44,6 +44,9 @@ bool good_strides(const int64_t* s, int d, int T) {
   return T == 1 || s[2] >= d;
 }
 
+// Of an output: no two rows in one place.
+bool rows_apart(const int64_t* s, int B, int H) { return (B == 1 || s[0] > 0) && (H == 1 || s[1] > 0); }
+
 sa_status check_rows(const sa_cache* c, int32_t layer, int32_t B, int32_t T, int32_t dtype,
                      bool lens) {
   const sa_status s = check_books(c, true, lens, false);
@@ -81,7 +84,7 @@ sa_status rows(const sa_cache* c, bool read, int32_t layer, int32_t B, int32_t T
   const sa_status s = check_rows(c, layer, B, T, dtype, !read);
   if (s != SA_OK) return s;
   if (!k || !v || (read && k == v) || !aligned(k, 16) || !aligned(v, 16) || !good_strides(stride, c->d, T) ||
-      !ints_or_null(slots) || !ints_or_null(starts) || !ints_or_null(counts) || (!read && !ints_or_null(c->refs)))
+      (read && !rows_apart(stride, B, c->Hkv)) || !ints_or_null(slots) || !ints_or_null(starts) || !ints_or_null(counts) || (!read && !ints_or_null(c->refs)))
     return SA_ERR_INVALID_ARG;
   int* status = cache_status_ptr();
   if (!status) return SA_ERR_CUDA;
@@ -141,7 +144,7 @@ sa_status sa_cache_attend(const sa_cache* c, int32_t layer, int32_t B, int32_t T
   if (!attend_fits(c, B, T, Hq)) return SA_ERR_UNSUPPORTED;
   if (!q || !y || q == y || !ws || !aligned(q, 16) || !aligned(y, 16) || !aligned(ws, 16) || !ints_or_null(lse) ||
       !ints_or_null(slots) || !ints_or_null(counts) || !good_strides(q_stride, c->d, T) ||
-      !good_strides(y_stride, c->d, T))
+      !good_strides(y_stride, c->d, T) || !rows_apart(y_stride, B, Hq))
     return SA_ERR_INVALID_ARG;
   if (ws_bytes < cache_attend_ws_bytes(B, T, Hq, c->Hkv, c->d, dtype)) return SA_ERR_WORKSPACE;
   int* status = cache_status_ptr();

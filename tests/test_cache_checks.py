@@ -6,7 +6,7 @@ import torch
 
 from paper_2604_00754_b200 import binding as sa
 from paper_2604_00754_b200.cache import KVCache
-from test_cache_host import FAKE, append, cache
+from test_cache_host import FAKE, OTHER, append, attend, cache
 
 
 def test_append_checks_the_holders_it_is_given():
@@ -105,3 +105,17 @@ def test_batches_past_32_bits_are_refused():
     for call in (lambda: sa.sa_cache_append(pool, table, lens, many, many), lambda: sa.sa_cache_attend(pool, table, lens, many)):
         with pytest.raises(ValueError, match="a dimension of 2.31 or more"):
             call()
+
+
+# ---- outputs whose rows share memory: which row stays would be chance
+
+@pytest.mark.parametrize("B,strides", [(2, (0, 128, 64)), (1, (1024, 0, 64)), (2, (0, 0, 64))])
+def test_outputs_that_share_memory_are_refused(B, strides):
+    st = (ctypes.c_int64 * 3)(*strides)
+    assert attend(cache(), B=B, ys=st) == 1
+    assert sa.load_library().sa_cache_read(ctypes.byref(cache()), 0, B, 1, FAKE, OTHER, sa.BF16, st, None, None, None, None) == 1
+
+
+def test_inputs_may_share_memory():
+    st = (ctypes.c_int64 * 3)(0, 0, 64)
+    assert attend(cache(), B=2, qs=st, ws_bytes=64) == 3            # as far as its workspace
