@@ -119,3 +119,136 @@ def test_outputs_that_share_memory_are_refused(B, strides):
 def test_inputs_may_share_memory():
     st = (ctypes.c_int64 * 3)(0, 0, 64)
     assert attend(cache(), B=2, qs=st, ws_bytes=64) == 3            # as far as its workspace
+
+
+# ---- what each Python call says of tensors that do not fit; a call without a fault gets as far as the device
+
+@pytest.fixture
+def t():
+    table, lens = books()
+    return dict(pool=sa.sa_cache_pool(1, 4, 2, 16, 64, device="cpu"), table=table, lens=lens,
+                refs=torch.zeros(4, dtype=torch.int32), x=rows(64), q=torch.zeros(2, 4, 1, 64, dtype=torch.bfloat16),
+                list=torch.zeros(2, dtype=torch.int32))
+
+
+POOL = r"pool must be contiguous uint8 \[layers, pages, Hkv, 2, page \* \(d/2 \+ d/16\)\]"
+TABLE, LENS = r"table must be contiguous int32 \[slots, row\]", r"lens must be contiguous int32 \[slots\]"
+LISTS = "counts must be contiguous int32"
+DEVICE = "must be on a CUDA device"
+
+
+def attend_of(t, **kw):
+    return sa.sa_cache_attend(t["pool"], t["table"], t["lens"], t["q"], **kw)
+
+
+def append_of(t, **kw):
+    return sa.sa_cache_append(t["pool"], t["table"], t["lens"], t["x"], t.get("v", t["x"]), **kw)
+
+
+def read_of(t, **kw):
+    return sa.sa_cache_read(t["pool"], t["table"], t["x"], t.get("v", t["x"]), **kw)
+
+
+def half(x):
+    return torch.cat((x, x), 1)[:, ::2]
+
+
+@pytest.mark.parametrize("name,change,text", [
+    ("pool", lambda x: x.int(), POOL), ("pool", lambda x: x[0], POOL), ("pool", half, POOL),
+    ("pool", lambda x: x[:, :, :, :1].contiguous(), POOL), ("table", lambda x: x.long(), TABLE),
+    ("table", half, TABLE), ("table", lambda x: x[0], TABLE)])
+def test_caches_that_do_not_fit_say_so(t, name, change, text):
+    t[name] = change(t[name])
+    for call in (attend_of, append_of, read_of):
+        with pytest.raises(ValueError, match=text):
+            call(t)
+
+
+@pytest.mark.parametrize("change", [lambda x: x.long(), lambda x: x[:1], lambda x: torch.stack((x, x), 1)[:, 0]])
+def test_lists_that_do_not_fit_say_so(t, change):
+    good, bad = t["list"], change(t["list"])
+    for call, names in ((attend_of, ("slots", "counts")), (append_of, ("slots", "counts")),
+                        (read_of, ("slots", "starts", "counts"))):
+        for name in names:
+            with pytest.raises(ValueError, match=LISTS):
+                call(t, **{name: bad})
+            with pytest.raises(ValueError, match=DEVICE):
+                call(t, **{name: good})
+    t["lens"] = bad
+    for call in (attend_of, append_of):
+        with pytest.raises(ValueError, match=LENS):
+            call(t)
+    with pytest.raises(ValueError, match=DEVICE):
+        read_of(t)                                           # looks at no lengths
+
+
+@pytest.mark.parametrize("x,v,text", [
+    (lambda x: x[0], lambda x: x[0], r"k and v must be \[B,Hkv,T,d\]"), (lambda x: x, lambda x: x[:1], r"k and v must be \[B,Hkv,T,d\]"),
+    (lambda x: x, lambda x: x.float(), r"k and v must be \[B,Hkv,T,d\]"),
+    (lambda x: half(x.transpose(1, 3)).transpose(1, 3), lambda x: half(x.transpose(1, 3)).transpose(1, 3), "head dimension must be contiguous"),
+    (lambda x: x, lambda x: torch.cat((x, x), 1)[:, :2], "k and v must share their strides"),
+    (lambda x: x[:, :1].contiguous(), lambda x: x[:, :1].contiguous(), "k and v must have the pool's heads")])
+def test_keys_and_values_that_do_not_fit_say_so(t, x, v, text):
+    t["x"], t["v"] = x(t["x"]), v(t["x"])
+    for call in (append_of, read_of):
+        with pytest.raises(ValueError, match=text):
+            call(t)
+
+
+def test_read_into_rows_that_share_memory_says_so(t):
+    t["x"] = t["v"] = t["x"][:1].expand(2, 2, 1, 64)
+    with pytest.raises(ValueError, match="an output shares memory between its rows"):
+        read_of(t)
+    with pytest.raises(ValueError, match=DEVICE):
+        append_of(t)                                         # broadcast inputs are fine
+
+
+@pytest.mark.parametrize("kw,text", [
+    (dict(y=torch.zeros(2, 4, 1, 64)), "y must have the shape and type of q"),
+    (dict(y=torch.zeros(2, 4, 2, 64, dtype=torch.bfloat16)), "y must have the shape and type of q"),
+    (dict(y=torch.zeros(2, 1, 1, 64, dtype=torch.bfloat16).expand(2, 4, 1, 64)), "an output shares memory between its rows"),
+    (dict(lse=torch.zeros(2, 4)), "lse must be contiguous float32"), (dict(lse=torch.zeros(2, 4, 1).double()), "lse must be contiguous float32"),
+    (dict(lse=torch.zeros(2, 4, 2)[..., :1]), "lse must be contiguous float32")])
+def test_outputs_of_attend_that_do_not_fit_say_so(t, kw, text):
+    with pytest.raises(ValueError, match=text):
+        attend_of(t, **kw)
+
+
+def test_queries_that_do_not_fit_say_so(t):
+    q = t["q"]
+    for bad, kind, text in ((q[0], ValueError, r"q must be \[B,Hq,T,d\]"), (q.half(), TypeError, "float32 or bfloat16"),
+                            (half(q.transpose(1, 3)).transpose(1, 3), ValueError, "head dimension must be contiguous"),
+                            (q[:, :3].contiguous(), sa.SaError, "sa_cache_attend")):
+        t["q"] = bad
+        with pytest.raises(kind, match=text):
+            attend_of(t)
+    t["q"] = q
+    with pytest.raises(ValueError, match=DEVICE):
+        attend_of(t)
+
+
+def test_books_that_do_not_fit_say_so(t):
+    table, lens, refs, two = t["table"], t["lens"], t["refs"], t["list"]
+    reserve = lambda **kw: sa.sa_cache_reserve(*((t | kw)[n] for n in ("pool", "table", "lens", "refs", "add")), 16, kw.get("got"))  # noqa: E731
+    t["add"] = two
+    REFS = r"refs must be contiguous int32 \[pages\]"
+    for kw, text in ((dict(refs=refs[:3]), REFS), (dict(refs=refs.long()), REFS), (dict(lens=lens[:1]), LENS), (dict(table=table.long()), TABLE),
+                     (dict(add=two[:1]), r"add must be contiguous int32 \[slots\]"), (dict(add=two.long()), r"add must be contiguous int32 \[slots\]"),
+                     (dict(got=two[:1]), r"got must be contiguous int32 \[slots\]"), (dict(got=two.float()), r"got must be contiguous int32 \[slots\]"),
+                     ({}, DEVICE)):
+        with pytest.raises(ValueError, match=text):
+            reserve(**kw)
+    for refs_, live, text in ((refs[:3], None, REFS), (refs, two, r"live must be int32 \[1\]"), (refs, None, DEVICE)):
+        with pytest.raises(ValueError, match=text):
+            sa.sa_cache_compact(t["pool"], table, refs_, live)
+    for a, b, text in ((two, two[:1], "parents and children must have one length"), (two.long(), two, "slot lists must be contiguous int32"),
+                       (two, two, DEVICE)):
+        with pytest.raises(ValueError, match=text):
+            sa.sa_cache_fork(table, lens, refs, a, b, page=16)
+    for slots, text in ((two.long(), "slot lists must be contiguous int32"), (two, DEVICE)):
+        with pytest.raises(ValueError, match=text):
+            sa.sa_cache_free(table, lens, refs, slots)
+    with pytest.raises(ValueError, match=r"refs must be contiguous int32 \[pages\]"):
+        append_of(t, refs=refs[:3])
+    with pytest.raises(ValueError, match=DEVICE):
+        append_of(t, refs=refs)
