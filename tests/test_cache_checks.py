@@ -6,7 +6,7 @@ import torch
 
 from paper_2604_00754_b200 import binding as sa
 from paper_2604_00754_b200.cache import KVCache
-from test_cache_host import FAKE, OTHER, append, attend, cache
+from test_cache_host import FAKE, ODD, OTHER, ST, append, attend, cache
 
 
 def test_append_checks_the_holders_it_is_given():
@@ -252,3 +252,21 @@ def test_books_that_do_not_fit_say_so(t):
         append_of(t, refs=refs[:3])
     with pytest.raises(ValueError, match=DEVICE):
         append_of(t, refs=refs)
+
+
+# ---- reads of the C library, k and v in two places
+
+@pytest.mark.parametrize("kw,expect", [
+    (dict(k=None), 1), (dict(v=None), 1), (dict(k=ODD), 1), (dict(v=ODD), 1), (dict(dt=5), 1), (dict(layer=7), 1),
+    (dict(layer=-1), 1), (dict(B=0), 1), (dict(T=0), 1), (dict(st=None), 1), (dict(st=(ctypes.c_int64 * 3)(1024, 100, 64)), 1),
+    (dict(st=(ctypes.c_int64 * 3)(-8, 128, 64)), 1), (dict(T=2, st=(ctypes.c_int64 * 3)(1024, 128, 56)), 1), (dict(B=1 << 17), 2),
+    (dict(T=1 << 30), 2), (dict(slots=0x1001), 1), (dict(starts=0x1002), 1), (dict(counts=0x1003), 1), (dict(v=FAKE), 1)])
+def test_read_refusals(kw, expect):
+    a = dict(layer=0, B=1, T=1, k=FAKE, v=OTHER, dt=sa.BF16, st=ST, slots=None, starts=None, counts=None) | kw
+    assert sa.load_library().sa_cache_read(ctypes.byref(cache(lens=None)), *a.values(), None) == expect
+
+
+@pytest.mark.parametrize("kw,expect", [(dict(pool=None), 1), (dict(pool=ODD), 1), (dict(table=None), 1), (dict(k_scale=0.3), 1),
+                                       (dict(v_scale=0.0), 1), (dict(page=24), 1), (dict(d=40), 2)])
+def test_reads_of_bad_caches_are_refused(kw, expect):
+    assert sa.load_library().sa_cache_read(ctypes.byref(cache(**kw)), 0, 1, 1, FAKE, OTHER, sa.BF16, ST, None, None, None, None) == expect
