@@ -404,8 +404,11 @@ sa_status sa_cache_fork(const sa_cache* c, int32_t n, const int32_t* parents,
 /* Makes room for add[s] tokens (device int32 [slots]) behind lens[s] in every slot: pages that are missing are
  * taken from the free ones, and pages of that range which others hold too are replaced by a copy of their
  * own, in all layers, before anything is written to them.  Free pages go out lowest first, to slots in
- * their order; a slot gets all that it needs or nothing, and once one did not fit none behind it gets any.
- * A page that all its holders replace in one call is free afterwards, for later calls.
+ * their order; a slot gets all that it needs or nothing, and once the free pages did not suffice for one, no
+ * slot behind it gets any.  A slot whose row is too short, or whose number or entries are bad, takes none and
+ * stands in no other's way.
+ * A page that all its holders replace in one call is copied for each and free afterwards, for later calls:
+ * two holders with one free page between them do not both go on.
  * got: out, device int32 [slots], not add: 1 where the room is there, 0 where it is not (no pages left, or
  * a row too short).  lens is not changed.  ws: scratch of sa_cache_ws_bytes(c), 16-byte aligned. */
 size_t sa_cache_ws_bytes(const sa_cache* c);

@@ -108,3 +108,18 @@ def test_a_captured_step_goes_on_through_a_full_pool(chunk, pages):
         for o, x in ((ko, kept[s][0]), (vo, kept[s][1])):
             assert np.array_equal(o[s, :, :books.lens[s]].double().cpu().numpy(), x)
     assert sa.sa_read_status() == 0
+
+
+# ---- who stands in whose way
+
+def test_a_row_that_is_too_short_takes_no_pages_and_stops_nobody():
+    """Pages running out stops the slots behind; a short row, a bad number and a bad entry do not, and take none."""
+    short, out = (sa.sa_cache_pool(1, 8, 1, 16, 16) for _ in range(2))
+    table = ints([[0, -1], [1, 99], [2, -1], [3, -1], [4, -1]])
+    refs, lens = ints([1, 1, 1, 1, 1, 0, 0, 0]), ints([16] * 5)
+    got = sa.sa_cache_reserve(short, table, lens, refs, ints([17, 1, -1, 1, 16]), page=16)
+    assert sa.sa_read_status() == 8 and got.tolist() == [0, 0, 0, 1, 1]
+    assert table.tolist() == [[0, -1], [1, 99], [2, -1], [3, 5], [4, 6]] and refs.tolist() == [1] * 7 + [0]
+    table, refs = ints([[0, -1, -1], [1, -1, -1], [2, -1, -1]]), ints([1] * 7 + [0])
+    got = sa.sa_cache_reserve(out, table, ints([16] * 3), refs, ints([17, 1, 0]), page=16)
+    assert sa.sa_read_status() == 0 and got.tolist() == [0, 0, 1] and refs.tolist() == [1] * 7 + [0]
