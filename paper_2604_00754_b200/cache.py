@@ -65,7 +65,9 @@ class KVCache:
                                   self.k_scale, self.v_scale, y, want_lse, lse, page=self.page)
 
     def read(self, layer: int, k, v, slots=None, starts=None, counts=None):
-        """Tokens starts[b] + t (from 0) of a layer into k, v: a cached prefix for a prefill that goes on from it."""
+        """Tokens starts[b] + t (from 0) of a layer into k, v: what ``attend`` sees of them.  (The forward calls take as many
+        queries as keys: a chunk goes on from a cached prefix through ``attend`` with flags 0, joined through lse with
+        the chunk's attention to itself.)"""
         return sa.sa_cache_read(self.pool, self.table, k, v, layer, slots, starts, counts, self.k_scale, self.v_scale,
                                 self.page)
 

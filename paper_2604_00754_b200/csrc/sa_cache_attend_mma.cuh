@@ -6,8 +6,8 @@
 // between HBM and the multiply has to keep up with 23 bytes = 41 values per clock and SM.  A warp takes 16
 // keys of each step alone, from its copies to its own running maximum, sum and rows: no barrier stands
 // in the loop, the four warps of a CTA join once per segment.
-// 32 sequences of 32768 keys, 32/8 heads of 128 (1.21 GB): 229 us, 82 % of the copy bandwidth (260 when the power cap holds
-// the clock at 1755 MHz).  What holds it back is the work itself: per warp and 16 keys of 128 dimensions 64
+// 32 sequences of 32768 keys, 32/8 heads of 128 (1.21 GB): 255-275 us, 68-73 % of the copy bandwidth, where the power cap
+// holds the clock near 1755 MHz; 236 (79 %) in the first calls of a burst.  What holds it back is the work itself: per warp and 16 keys of 128 dimensions 64
 // conversions, 64 products with scales, 16 matrix instructions and 160 others, the ALU half busy, three warps per
 // scheduler.
 //   - Copies: cp.async into a ring of the warp's own (pages are contiguous per head and side: 16-byte pieces).
@@ -120,9 +120,11 @@ struct Shape {
   static constexpr int kTurns = kUnits == 2 ? (D == 64 ? 3 : 2) : D == 64 ? 6 : D == 128 ? 4 : 3;
   static constexpr int kRing = kTurns * kUnits * Tile<D>::kBytes;
   // CTAs per SM: what registers (rows of O, Q, the tile in flight) and shared memory leave.  With 64 registers of O
-  // two CTAs without spills beat three with them in one tile of rows and in four (16 x 8192 keys, 16/4 heads of 256
-  // 45.9 against 46.8 us; four tiles of fp32 rows over 9 x 2500 keys of 16 heads of 64 64.8 against 70.7), not in
-  // two (four tokens over 16 x 8192 keys, 32/8 heads of 128: 67.1 against 64.2).
+  // two CTAs are as good as three in one tile of rows or better (16 x 8192 keys, 16/4 heads of 256: bf16 43.5 us
+  // against 43.2, fp32 57.0 against 59.6) and as good in four (32 fp32 rows over 9 x 2500 keys of 16 heads of 64:
+  // 47.5 against 47.4), not in two (four tokens over 16 x 8192 keys, 32/8 heads of 128: 67.1 against 64.2).  Some fp32
+  // instances spill at that: one tile of 128 dimensions 56 bytes of a thread at three CTAs, which beat two without
+  // spills (16 x 8192 keys, 32/8 heads: 54.3 against 56.7); two tiles of 256 dimensions 116, of 64 dimensions 56.
   static constexpr int kORegs = kKs * 4 * NT;
   static constexpr int kCtas = kORegs + (kQInRegs ? kKs * 2 * NT * PC : 0) <= 40 ? 4
                                : kORegs < 64 || (kORegs == 64 && NT == 2) ? 3 : 2;

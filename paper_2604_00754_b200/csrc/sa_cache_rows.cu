@@ -15,7 +15,8 @@
 // Bound by HBM as long as few instructions stand between: a CTA takes one head and side, a thread keeps its
 // place within the row and moves on by whole rows; t is folded into y and s; the tensors' 32 bytes of a thread (64
 // in fp32) go in whole sectors by 32-byte accesses where they are aligned to that.  32768 tokens of 8 heads of 128 in
-// bf16, 172 MB each way: append 33 us (81 % of the copy bandwidth), read 31 (86 %).
+// bf16, 172 MB each way: append 32-33 us (81 % of the copy bandwidth; 33.1 where it looks at the pages' holders, a
+// load that the tokens of a page share in L1), read 31 (86 %).
 #include "sa_cache.cuh"
 
 namespace sa {
